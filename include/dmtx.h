@@ -261,6 +261,131 @@ int attn_input_bias_grad(int32_t dtype, int64_t rows, int32_t H, int32_t P, cons
 int residual_add(int32_t dtype, int64_t n, const void* a, const void* b, void* out,
                  void* stream);
 
+/* ------------------------------------------- streaming attention
+ * Attention over given queries, keys and values (projections are the
+ * caller's; mha_fwd has them built in) that stores no [J][K] tensor: one
+ * pass over the keys with a running softmax, the probabilities formed again
+ * in the backward.  Scores may be capped or get a bias that falls with the
+ * distance, and masks may leave any query any set of keys:
+ *   s = scaler q.k;  s = cap tanh(s / cap) if cap > 0;  s -= slopes[h] |p - k|;
+ *   out = sum_k softmax_k(s) v over the keys the query sees; zeros if none.
+ * Query j of sequence b has position p = k_len - q_len + j (the last query
+ * stands at the last key), key k position k.  The query sees key k if
+ *   j < q_len, k < k_len, and
+ *   causal: k <= p, or k < prefix[b];  and
+ *   doc: doc[b][p] == doc[b][k] >= 0 (a query outside 0 .. k_len-1 sees none).
+ * Rows outside their sequence's length (k >= k_len, j >= q_len) and keys with
+ * a negative document id are not read: they may hold anything.  All other
+ * elements of q, k, v and dout have to be finite (a key that is hidden from
+ * one query only by causal or by its document takes part as 0 times its
+ * value).  Query head h reads key/value head h / (H / G).
+ * One entry point covers training, prompts and single tokens (J = 1 over a
+ * cache of K keys, of which sequence b holds k_len[b]).
+ * The descriptor's device arrays are read by the call's kernels.  Sizes may
+ * be 0 (B, J: nothing to do; K: zeros).  Results do not depend on the run:
+ * nothing is summed by atomics. */
+
+/* Element (b, head, token, d) sits at b*b + head*h + token*t + d elements;
+ * strides are multiples of 8, not negative, and those of written tensors do
+ * not overlap (0 is allowed for k and v that are only read). */
+typedef struct {
+    int64_t b, h, t;
+} dm_attn_stride;
+
+typedef struct {
+    int32_t B, J, K;         /* sequences, queries and keys (capacity) of each             */
+    int32_t H, G;            /* query heads; key/value heads (H a multiple of G)           */
+    int32_t P;               /* head size: a multiple of 8 up to 128                       */
+    int32_t dtype;           /* dm_dtype of all tensors; scores and sums are fp32, and     */
+                             /* probabilities enter the products in the storage type       */
+    float scaler;            /* <= 0 selects 1/sqrt(P)                                     */
+    float cap;               /* 0: none                                                    */
+    int32_t causal;          /* 0 or 1                                                     */
+    dm_attn_stride q, k, v, out;  /* dq, dk, dv, dout as q, k, v, out                      */
+    const int32_t* q_len;    /* device [B] or NULL: J                                      */
+    const int32_t* k_len;    /* device [B] or NULL: K                                      */
+    const int32_t* doc;      /* device [B][K] or NULL: document of each position           */
+    const int32_t* prefix;   /* device [B] or NULL; needs causal                           */
+    const float* slopes;     /* device [H] or NULL                                         */
+} dm_attn_desc;
+
+/* Bytes of `saved` (forward to backward, opaque) and of the workspaces;
+ * any of the outputs may be NULL.  The sizes depend on the descriptor's
+ * sizes and on whether doc is given. */
+int attn_sizes(const dm_attn_desc* d, size_t* saved_bytes, size_t* fwd_ws_bytes,
+               size_t* bwd_ws_bytes);
+
+/* out of every query row (rows j >= q_len: zeros).  saved: NULL when no
+ * backward follows. */
+int attn_fwd(const dm_attn_desc* d, const void* q, const void* k, const void* v, void* out,
+             void* saved, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients of q, k and v from dout and the forward's out and saved; every
+ * row is written (those outside their sequence's length: zeros).  slopes
+ * and masks are constants. */
+int attn_bwd(const dm_attn_desc* d, const void* q, const void* k, const void* v, const void* out,
+             const void* saved, const void* dout, void* dq, void* dk, void* dv, void* ws,
+             size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------- embedding
+ * y[t] = scale * table[ids[t]] over tokens x cols (table [vocab][cols]; ids
+ * device int32).  An id outside 0 .. vocab-1 gives zeros.  cols up to 16384. */
+int embed_fwd(int32_t dtype, int64_t tokens, int32_t vocab, int32_t cols, const int32_t* ids,
+              const void* table, float scale, void* y, void* stream);
+
+/* dtable[v] = scale * sum over ids[t] == v of dy[t] (float [vocab][cols], all
+ * of it written; zeros for ids that do not occur, and for pad_id, whose
+ * tokens have no gradient: -1 = none).  Ids outside 0 .. vocab-1 are left
+ * out.  Sums run in an order given by the ids alone.  ws of
+ * embed_ws_bytes(tokens, vocab, cols) bytes (may be 0). */
+size_t embed_ws_bytes(int64_t tokens, int32_t vocab, int32_t cols);
+int embed_bwd(int32_t dtype, int64_t tokens, int32_t vocab, int32_t cols, const int32_t* ids,
+              int32_t pad_id, const void* dy, float scale, float* dtable, void* ws, size_t ws_bytes,
+              void* stream);
+
+/* ------------------------------------------------- optimiser step
+ * One AdamW step over any number of tensors (the weights of all layers, say,
+ * with the float32 gradients that the backward calls write), in one launch
+ * for every 44 of them:
+ *   g = grad_scale * grad;  m = beta1 m + (1 - beta1) g;
+ *   v = beta2 v + (1 - beta2) g^2;
+ *   w = w (1 - lr decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * in float32, each operation rounded by itself.  w is the tensor's fp32
+ * master copy, of which param gets the rounded value; without one, param
+ * itself.  Tensors of a call have a master copy all or none, and do not
+ * overlap.
+ * state_bits = 32: m and v are float [n].  state_bits = 8: m holds e4m3 codes
+ * (OCP, one byte) of m / m_scale, v those of sqrt(v) / v_scale, with a float
+ * scale for each 256 elements, the block's largest value / 448 (zero, and
+ * codes of zero, for a block below 2^-100); a root that is not zero keeps at
+ * least the smallest code.  The step itself uses m and v before that
+ * rounding.  Zeros in codes and scales are the states of a first step. */
+typedef struct {
+    void* param;             /* [n], dtype                                     */
+    float* master;           /* [n] or NULL                                    */
+    const float* grad;       /* [n]                                            */
+    void *m, *v;             /* [n], float or codes                            */
+    float *m_scale, *v_scale;/* [(n + 255) / 256]; NULL for states in 32 bits  */
+    int64_t n;               /* 0: the tensor is left out                      */
+    double decay;            /* weight decay, >= 0                             */
+} dm_adamw_tensor;
+
+typedef struct {
+    int32_t dtype;           /* dm_dtype of param                              */
+    int32_t state_bits;      /* 32 or 8                                        */
+    double lr, beta1, beta2, eps;
+    double grad_scale;       /* 1: gradients as they are                       */
+    int64_t step;            /* 1 for the first                                */
+    const float* scalars;    /* NULL, or device float[4] (16-byte aligned): lr,*/
+                             /* 1/(1-beta1^step), 1/(1-beta2^step), grad_scale,*/
+                             /* read when the kernels run, in place of the     */
+                             /* fields above (a step captured into a graph     */
+                             /* replays with what the array holds then)        */
+} dm_adamw_desc;
+
+/* tensors: host array, copied into the launches. */
+int adamw_step(const dm_adamw_desc* a, const dm_adamw_tensor* tensors, int32_t count, void* stream);
+
 /* ------------------------------------------------------ test hooks */
 
 /* Keep bits (0/1 bytes) of logical elements offset .. offset+n-1 of a

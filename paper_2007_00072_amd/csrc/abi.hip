@@ -8,8 +8,8 @@
 #include <new>
 #include <vector>
 
+#include "checks.hpp"
 #include "gemm.hpp"
-#include "internal.hpp"
 
 namespace dm {
 
@@ -107,45 +107,6 @@ DropParams make_drop(float p, uint64_t seed, uint32_t site, uint32_t layer) {
 }  // namespace dm
 
 using namespace dm;
-
-namespace {
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
-int check_ptr(const void* p, const char* name) {
-    if (!p) return set_error(DM_ERR_ARG, "%s is NULL", name);
-    if (!aligned16(p)) return set_error(DM_ERR_ARG, "%s is not 16-byte aligned", name);
-    return DM_OK;
-}
-
-int check_dtype(int32_t dt) {
-    if (dt != DM_F32 && dt != DM_F16 && dt != DM_BF16)
-        return set_error(DM_ERR_UNSUPPORTED, "unsupported dtype %d", dt);
-    return DM_OK;
-}
-
-int check_drop(const dm_dropout* d) {
-    if (d && !(d->p >= 0.f && d->p < 1.f)) return set_error(DM_ERR_ARG, "dropout p=%g outside [0,1)", d->p);
-    return DM_OK;
-}
-
-int check_rows(int64_t rows, int32_t cols, int32_t max_cols) {
-    if (rows < 0 || cols <= 0) return set_error(DM_ERR_ARG, "bad shape rows=%lld cols=%d", (long long)rows, cols);
-    if (cols % 8) return set_error(DM_ERR_UNSUPPORTED, "row length %d is not a multiple of 8", cols);
-    if (max_cols && cols > max_cols) return set_error(DM_ERR_UNSUPPORTED, "row length %d above %d", cols, max_cols);
-    if (rows > (int64_t)INT32_MAX * 8) return set_error(DM_ERR_UNSUPPORTED, "too many rows");
-    return DM_OK;
-}
-
-#define DM_TRY(x)                      \
-    do {                               \
-        int _rc = (x);                 \
-        if (_rc != DM_OK) return _rc;  \
-    } while (0)
-
-hipStream_t S(void* s) { return reinterpret_cast<hipStream_t>(s); }
-
-}  // namespace
 
 extern "C" {
 

@@ -1,0 +1,208 @@
+// Host side of attention without a [J][K] tensor: descriptor checks,
+// workspace layout and the choice of the forward's form.
+#include <math.h>
+
+#include "checks.hpp"
+#include "stream.hpp"
+
+namespace dm {
+namespace {
+
+constexpr size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+size_t esize(int dtype) { return dtype == DM_F32 ? 4 : 2; }
+
+// Query heads that share a key/value head lie side by side in a row tile
+// where the queries alone would leave it part empty.
+int packed_heads(const dm_attn_desc& d) { return d.J < STREAM_BM ? d.H / d.G : 1; }
+
+// Few rows of a key/value head (single tokens): the waves of a block share
+// 32 rows and walk keys of their own.
+bool few_rows(const dm_attn_desc& d) { return (int64_t)d.J * packed_heads(d) <= 2 * STREAM_BM_FEW; }
+
+// Parts the keys are split into, so that the GPU's 256 CUs have two blocks
+// each where the rows alone give fewer, while a part has some steps to walk.
+int key_splits(const dm_attn_desc& d) {
+    const bool few = few_rows(d);
+    const int64_t bm = few ? STREAM_BM_FEW : STREAM_BM, bn = few ? STREAM_BN_FEW : STREAM_BN;
+    const int64_t pack = packed_heads(d);
+    const int64_t blocks = ((int64_t)d.J * pack + bm - 1) / bm * d.B * (d.H / pack);
+    const int64_t steps = (d.K + bn - 1) / bn, least = few ? 2 : 4;
+    if (blocks == 0 || blocks >= 384) return 1;
+    int64_t s = (512 + blocks - 1) / blocks;
+    if (s > steps / least) s = steps / least;
+    return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+}
+
+struct Sizes {
+    size_t lo, saved;                     // saved: lse, then lo
+    size_t ranges, part_o, part_ml, fwd;  // forward workspace: ends of its parts
+    size_t dsum, dmax, bwd;               // backward workspace (ranges first)
+    int splits, dmax_n;
+};
+
+Sizes sizes_of(const dm_attn_desc& d) {
+    Sizes s{};
+    const size_t rows = (size_t)d.B * d.H * d.J;
+    s.lo = align256(rows * 4);
+    s.saved = s.lo + (d.dtype == DM_F32 ? 0 : align256(rows * d.P * esize(d.dtype)));
+    s.ranges = d.doc ? align256((size_t)d.B * ((d.K + STREAM_RANGE - 1) / STREAM_RANGE) * sizeof(int2)) : 0;
+    s.splits = key_splits(d);
+    const size_t parts = s.splits > 1 ? (size_t)s.splits * rows : 0;
+    s.part_o = s.ranges + align256(parts * d.P * 4);
+    s.part_ml = s.part_o + align256(parts * 8);
+    s.fwd = s.part_ml;
+    s.dmax_n = (d.J + STREAM_DROWS - 1) / STREAM_DROWS;
+    s.dsum = s.ranges + align256(rows * 4);
+    s.dmax = s.dsum + (d.dtype == DM_F16 ? align256((size_t)d.B * d.H * s.dmax_n * 4) : 0);
+    s.bwd = s.dmax;
+    return s;
+}
+
+int check_stride(const dm_attn_stride& s, const char* n) {
+    if (s.b < 0 || s.h < 0 || s.t < 0) return set_error(DM_ERR_UNSUPPORTED, "%s: negative stride", n);
+    if (s.b % 8 || s.h % 8 || s.t % 8)
+        return set_error(DM_ERR_UNSUPPORTED, "%s: strides must be multiples of 8 elements", n);
+    return DM_OK;
+}
+
+// a tensor that is written: no element twice, as far as strides tell (sorted
+// by size, each steps over what the smaller ones span)
+int check_written(const dm_attn_stride& s, int64_t nb, int64_t nh, int64_t nt, int64_t P, const char* n) {
+    int64_t st[3] = {s.b, s.h, s.t}, len[3] = {nb, nh, nt};
+    if (nb == 0 || nh == 0 || nt == 0) return DM_OK;
+    for (int i = 0; i < 2; ++i)
+        for (int k = 0; k < 2 - i; ++k)
+            if (st[k] > st[k + 1]) {
+                const int64_t a = st[k], c = len[k];
+                st[k] = st[k + 1]; len[k] = len[k + 1];
+                st[k + 1] = a; len[k + 1] = c;
+            }
+    int64_t span = P;
+    for (int i = 0; i < 3; ++i) {
+        if (len[i] <= 1) continue;
+        if (st[i] < span) return set_error(DM_ERR_UNSUPPORTED, "%s: strides let elements overlap", n);
+        span = st[i] * (len[i] - 1) + span;
+    }
+    return DM_OK;
+}
+
+int check_desc(const dm_attn_desc* d) {
+    if (!d) return set_error(DM_ERR_ARG, "descriptor is NULL");
+    DM_TRY(check_dtype(d->dtype));
+    if (d->B < 0 || d->J < 0 || d->K < 0) return set_error(DM_ERR_ARG, "negative size");
+    if (d->H <= 0 || d->G <= 0 || d->H % d->G)
+        return set_error(DM_ERR_ARG, "H=%d heads are no multiple of G=%d key/value heads", d->H, d->G);
+    if (d->P <= 0 || d->P % 8 || d->P > 128)
+        return set_error(DM_ERR_UNSUPPORTED, "head size P=%d is not a multiple of 8 up to 128", d->P);
+    if ((int64_t)d->B * d->H * d->J > INT32_MAX || (int64_t)d->B * d->G * d->K > INT32_MAX || d->J > (1 << 30) ||
+        d->K > (1 << 30) || (int64_t)d->H * d->J > INT32_MAX || (int64_t)d->B * d->H > INT32_MAX / 64)
+        return set_error(DM_ERR_UNSUPPORTED, "B=%d H=%d G=%d J=%d K=%d: more than 2^31 - 1 rows", d->B, d->H, d->G, d->J,
+                         d->K);
+    if (!isfinite(d->scaler) || !isfinite(d->cap) || d->cap < 0.f)
+        return set_error(DM_ERR_ARG, "scaler=%g cap=%g", d->scaler, d->cap);
+    if (d->causal != 0 && d->causal != 1) return set_error(DM_ERR_ARG, "causal=%d", d->causal);
+    if (d->prefix && !d->causal) return set_error(DM_ERR_ARG, "prefix without causal: every key is seen already");
+    DM_TRY(check_stride(d->q, "q"));
+    DM_TRY(check_stride(d->k, "k"));
+    DM_TRY(check_stride(d->v, "v"));
+    DM_TRY(check_stride(d->out, "out"));
+    return check_written(d->out, d->B, d->H, d->J, d->P, "out");
+}
+
+StreamRows rows_of(const void* p, const dm_attn_stride& s) { return {(char*)p, s.b, s.h, s.t}; }
+
+StreamArgs args_of(const dm_attn_desc& d) {
+    StreamArgs a{};
+    a.B = d.B; a.J = d.J; a.K = d.K; a.H = d.H; a.G = d.G; a.P = d.P;
+    a.pack = packed_heads(d);
+    a.scaler = d.scaler > 0.f ? d.scaler : 1.f / sqrtf((float)d.P);
+    a.cap = d.cap;
+    a.causal = d.causal;
+    a.q_len = d.q_len; a.k_len = d.k_len; a.doc = d.doc; a.prefix = d.prefix; a.slopes = d.slopes;
+    a.splits = 1;
+    return a;
+}
+
+}  // namespace
+}  // namespace dm
+
+using namespace dm;
+
+extern "C" {
+
+int attn_sizes(const dm_attn_desc* d, size_t* saved_bytes, size_t* fwd_ws_bytes, size_t* bwd_ws_bytes) {
+    DM_TRY(check_desc(d));
+    const Sizes s = sizes_of(*d);
+    if (saved_bytes) *saved_bytes = s.saved;
+    if (fwd_ws_bytes) *fwd_ws_bytes = s.fwd;
+    if (bwd_ws_bytes) *bwd_ws_bytes = s.bwd;
+    return DM_OK;
+}
+
+int attn_fwd(const dm_attn_desc* d, const void* q, const void* k, const void* v, void* out, void* saved, void* ws,
+             size_t ws_bytes, void* stream) {
+    DM_TRY(check_desc(d));
+    if (d->B == 0 || d->J == 0) return DM_OK;
+    const Sizes s = sizes_of(*d);
+    DM_TRY(check_ptr(q, "q"));
+    if (d->K > 0) {
+        DM_TRY(check_ptr(k, "k"));
+        DM_TRY(check_ptr(v, "v"));
+    }
+    DM_TRY(check_ptr(out, "out"));
+    if (saved) DM_TRY(check_ptr(saved, "saved"));
+    if (ws_bytes < s.fwd) return set_error(DM_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws_bytes, s.fwd);
+    if (s.fwd) DM_TRY(check_ptr(ws, "ws"));
+    StreamArgs a = args_of(*d);
+    a.q = rows_of(q, d->q); a.k = rows_of(k, d->k); a.v = rows_of(v, d->v); a.o = rows_of(out, d->out);
+    if (saved) {
+        a.lse = (float*)saved;
+        if (d->dtype != DM_F32) a.lo = (char*)saved + s.lo;
+    }
+    a.ranges = (int2*)ws;
+    a.splits = s.splits;
+    a.part_o = (float*)((char*)ws + s.ranges);
+    a.part_ml = (float2*)((char*)ws + s.part_o);
+    const hipStream_t st = S(stream);
+    const bool few = few_rows(*d);
+    if (d->dtype == DM_F16) stream_fwd<half_t>(a, few, st);
+    else if (d->dtype == DM_BF16) stream_fwd<bf16_t>(a, few, st);
+    else stream_fwd<float>(a, few, st);
+    return check_launch("attn_fwd");
+}
+
+int attn_bwd(const dm_attn_desc* d, const void* q, const void* k, const void* v, const void* out, const void* saved,
+             const void* dout, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes, void* stream) {
+    DM_TRY(check_desc(d));
+    DM_TRY(check_written(d->q, d->B, d->H, d->J, d->P, "dq"));
+    DM_TRY(check_written(d->k, d->B, d->G, d->K, d->P, "dk"));
+    DM_TRY(check_written(d->v, d->B, d->G, d->K, d->P, "dv"));
+    if (d->B == 0) return DM_OK;
+    const Sizes s = sizes_of(*d);
+    if (d->J > 0) {
+        DM_TRY(check_ptr(q, "q")); DM_TRY(check_ptr(out, "out")); DM_TRY(check_ptr(saved, "saved"));
+        DM_TRY(check_ptr(dout, "dout")); DM_TRY(check_ptr(dq, "dq"));
+    }
+    if (d->K > 0) {
+        DM_TRY(check_ptr(k, "k")); DM_TRY(check_ptr(v, "v"));
+        DM_TRY(check_ptr(dk, "dk")); DM_TRY(check_ptr(dv, "dv"));
+    }
+    if (ws_bytes < s.bwd) return set_error(DM_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws_bytes, s.bwd);
+    if (s.bwd) DM_TRY(check_ptr(ws, "ws"));
+    StreamArgs a = args_of(*d);
+    a.q = rows_of(q, d->q); a.k = rows_of(k, d->k); a.v = rows_of(v, d->v); a.o = rows_of(out, d->out);
+    a.dout = rows_of(dout, d->out); a.dq = rows_of(dq, d->q); a.dk = rows_of(dk, d->k); a.dv = rows_of(dv, d->v);
+    a.lse = (float*)saved;
+    if (d->dtype != DM_F32) a.lo = (char*)saved + s.lo;
+    a.ranges = (int2*)ws;
+    a.dsum = (float*)((char*)ws + s.ranges);
+    a.dmax = d->dtype == DM_F16 ? (float*)((char*)ws + s.dsum) : nullptr;
+    a.dmax_n = s.dmax_n;
+    const hipStream_t st = S(stream);
+    if (d->dtype == DM_F16) stream_bwd<half_t>(a, st);
+    else if (d->dtype == DM_BF16) stream_bwd<bf16_t>(a, st);
+    else stream_bwd<float>(a, st);
+    return check_launch("attn_bwd");
+}
+
+}  // extern "C"

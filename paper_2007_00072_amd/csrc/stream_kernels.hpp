@@ -1,0 +1,981 @@
+// Kernels of attention without a [J][K] tensor.
+//
+// One pass over the keys with a running row maximum m and sum l: with scores
+// s in units of log2, m' = max(m, max s), p = 2^(s - m'), l' = l 2^(m - m') +
+// sum p, o' = o 2^(m - m') + p v; at the end o / l.  The backward recomputes
+// p = 2^(s - lse) from the saved lse = m + log2 l, and with the row term
+// D = dout . out: ds = p (dout . v - D) (1 - tanh^2 where scores are capped),
+// dq = scaler ds k, dk = scaler ds^T q, dv = p^T dout.
+//
+// All products run on 32x32x16 MFMAs (32x32x2 in float32), transposed so
+// that what the softmax needs per row lies in one lane: the first product
+// gives a lane one query (its column) and 16 of 32 keys (its accumulators),
+// so row maxima and sums are in-lane but for one exchange between the two
+// lane halves, and the accumulators, converted in place, are the second
+// product's operand: the order of a contraction is free, so its other
+// operand is read in the order the accumulators have (a lane half holds keys
+// 4 hh + {0..3, 8..11} of 16).  The dK / dV kernel does the same with keys
+// and queries exchanged.
+#pragma once
+
+#include <math.h>
+
+#include "stream.hpp"
+
+namespace dm {
+namespace stream {
+
+constexpr int NT = 256;  // threads of a block: 4 waves
+constexpr float LOG2E = 1.4426950408889634f;
+
+// ------------------------------------------------------------- fragments
+// 8 contraction elements of one row (or column) of an MFMA operand
+template <typename T> struct Frag { u32x4 v[sizeof(T) / 2]; };
+
+template <typename T> __device__ __forceinline__ floatx16 mma(const Frag<T>& a, const Frag<T>& b, floatx16 c);
+template <> __device__ __forceinline__ floatx16 mma(const Frag<half_t>& a, const Frag<half_t>& b, floatx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a.v[0]), __builtin_bit_cast(half8, b.v[0]),
+                                                  c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ floatx16 mma(const Frag<bf16_t>& a, const Frag<bf16_t>& b, floatx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.v[0]),
+                                                   __builtin_bit_cast(bf16x8, b.v[0]), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ floatx16 mma(const Frag<float>& a, const Frag<float>& b, floatx16 c) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const floatx4 x = __builtin_bit_cast(floatx4, a.v[k]), y = __builtin_bit_cast(floatx4, b.v[k]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], c, 0, 0, 0);
+    }
+    return c;
+}
+
+template <typename T> __device__ __forceinline__ Frag<T> frag_zero() {
+    Frag<T> f;
+#pragma unroll
+    for (auto& x : f.v) x = u32x4{0, 0, 0, 0};
+    return f;
+}
+template <typename T> __device__ __forceinline__ Frag<T> frag_load(const T* p) {
+    Frag<T> f;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) f.v[i] = reinterpret_cast<const u32x4*>(p)[i];
+    return f;
+}
+// accumulators 8 c .. 8 c + 7 as the operand of the next product, rounded to
+// the storage type (what the MFMA takes; sums stay in 32 bits)
+template <typename T> __device__ __forceinline__ Frag<T> frag_acc(const float* x) {
+    Frag<T> f;
+    if constexpr (sizeof(T) == 2) {
+        f.v[0] = V8<T>::pack(x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f.v[i >> 2][i & 3] = __builtin_bit_cast(uint32_t, x[i]);
+    }
+    return f;
+}
+
+// ------------------------------------------------------------- LDS tiles
+// Rows of PITCH bytes (a power of two, at least the padded head size); the
+// 16-byte pieces of row r are permuted by piece ^ f(r), with f such that the
+// 16 lanes that read one piece of 16 rows, and the lanes that read 4 pieces
+// of 4 rows with the transposing read, each reach all 64 banks once.
+template <int PITCH> __device__ __forceinline__ int swz(int r) {
+    if constexpr (PITCH == 64) return (r >> 2) & 3;
+    if constexpr (PITCH == 128) return ((r & 2) << 1) + ((r >> 2) & 3);
+    return 4 * (r & 3) + ((r >> 2) & 3);
+}
+template <int PITCH> __device__ __forceinline__ int piece_off(int r, int piece) {
+    return r * PITCH + ((piece ^ swz<PITCH>(r)) << 4);
+}
+
+template <typename T, int DP> struct Tile {
+    static constexpr int PITCH = DP * (int)sizeof(T);
+    static constexpr int PIECES = PITCH / 16;       // of a row
+    static constexpr int EPP = 16 / (int)sizeof(T);  // elements of a piece
+    typedef short s4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s4 lds_s4;
+
+    // elements e .. e + 7 of row r
+    static __device__ __forceinline__ Frag<T> row(const char* t, int r, int e) {
+        Frag<T> f;
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(T) / 2); ++i)
+            f.v[i] = *reinterpret_cast<const u32x4*>(t + piece_off<PITCH>(r, e / EPP + i));
+        return f;
+    }
+    // column c + lane % 32, rows r + 4 hh + {0..3, 8..11} (hh: lane half)
+    static __device__ __forceinline__ Frag<T> col(const char* t, int r, int c, int lane) {
+        Frag<T> f;
+        if constexpr (sizeof(T) == 2) {
+            // 16 lanes of a transposing read take 4 rows of 16 columns
+            const int sl = lane & 15, cc = c + 16 * ((lane >> 4) & 1) + 4 * (sl & 3);
+            const int rr = r + 4 * (lane >> 5) + (sl >> 2);
+            const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s4*)(t + piece_off<PITCH>(rr, cc >> 3) + (cc & 7) * 2));
+            const s4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s4*)(t + piece_off<PITCH>(rr + 8, cc >> 3) + (cc & 7) * 2));
+            const u32x2 lo = __builtin_bit_cast(u32x2, a), hi = __builtin_bit_cast(u32x2, b);
+            f.v[0] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+        } else {
+            const int cc = c + (lane & 31), rr = r + 4 * (lane >> 5);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                f.v[i >> 2][i & 3] = *reinterpret_cast<const uint32_t*>(
+                    t + piece_off<PITCH>(rr + (i & 3) + 8 * (i >> 2), cc >> 2) + (cc & 3) * 4);
+        }
+        return f;
+    }
+};
+
+// One step's rows of a tensor on their way from memory to a tile: requested
+// together, stored once the tile is free.  Rows that no query (or key) may
+// use are zeros whatever memory holds there.
+template <typename T, int DP, int ROWS> struct Stage {
+    using TL = Tile<T, DP>;
+    static constexpr int N = ROWS * TL::PIECES / NT;
+    static_assert(ROWS * TL::PIECES % NT == 0, "pieces");
+    u32x4 x[N];
+    // ok(row): the row holds data; rows count from `base`
+    template <typename Ok, typename At>
+    __device__ __forceinline__ void load(int tid, int P, Ok ok, At at) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = tid + i * NT, r = p / TL::PIECES, c = p % TL::PIECES;
+            x[i] = u32x4{0, 0, 0, 0};
+            if (c * TL::EPP < P && ok(r)) x[i] = *reinterpret_cast<const u32x4*>(at(r) + c * TL::EPP);
+        }
+    }
+    __device__ __forceinline__ void store(int tid, char* t) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = tid + i * NT;
+            *reinterpret_cast<u32x4*>(t + piece_off<TL::PITCH>(p / TL::PIECES, p % TL::PIECES)) = x[i];
+        }
+    }
+};
+
+// --------------------------------------------------------------- scores
+// 4 elements, rounded
+template <typename T> __device__ __forceinline__ void store4(T* p, const float* y) {
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<T4*>(p) = T4{from_f<T>(y[0]), from_f<T>(y[1]), from_f<T>(y[2]), from_f<T>(y[3])};
+}
+// the other lane half's value
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+
+// tanh for the capped scores: from one exponential in the 16-bit types
+// (absolute error about 1e-7, far under their resolution), the library's in
+// float32
+template <typename T> __device__ __forceinline__ float cap_tanh(float x) {
+    if constexpr (sizeof(T) == 2)
+        return 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * LOG2E)) + 1.f);
+    return tanhf(x);
+}
+
+// Which keys a query sees.  A causal query at position p sees keys 0 .. p,
+// and keys below the sequence's prefix: all keys below `hi`, of which its
+// own document's.
+struct Seq {
+    int q_len, k_len, off, prefix;  // off: position of query 0
+    __device__ __forceinline__ Seq(const StreamArgs& g, int b) {
+        k_len = g.k_len ? min(max(g.k_len[b], 0), g.K) : g.K;
+        q_len = g.q_len ? min(max(g.q_len[b], 0), g.J) : g.J;
+        off = k_len - q_len;
+        prefix = g.causal && g.prefix ? g.prefix[b] : 0;
+    }
+    __device__ __forceinline__ int hi(const StreamArgs& g, int j) const {
+        if (j >= q_len) return 0;
+        return g.causal ? min(k_len, max(off + j + 1, prefix)) : k_len;
+    }
+    // document of query j (-1: none)
+    __device__ __forceinline__ int doc_of(const StreamArgs& g, int b, int j) const {
+        const int p = off + j;
+        return j < q_len && p >= 0 && p < k_len ? g.doc[(int64_t)b * g.K + p] : -1;
+    }
+};
+
+// document ids of 64 keys: smallest and largest (an entry without any: none matches)
+__device__ __forceinline__ bool ranges_meet(int2 a, int2 b) { return a.x <= b.y && b.x <= a.y; }
+
+// 64 ids to (smallest, largest) of those that are documents
+__device__ __forceinline__ int2 wave_range(int id) {
+    int lo = id >= 0 ? id : INT32_MAX, hi = id >= 0 ? id : -1;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        lo = min(lo, __shfl_xor(lo, s, 64));
+        hi = max(hi, __shfl_xor(hi, s, 64));
+    }
+    return int2{__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(hi)};
+}
+
+template <typename T>
+__global__ __launch_bounds__(64) void ranges_k(StreamArgs g) {
+    const int nr = (g.K + STREAM_RANGE - 1) / STREAM_RANGE, b = (int)blockIdx.x / nr, e = (int)blockIdx.x - b * nr;
+    const int k = e * STREAM_RANGE + (int)threadIdx.x;
+    const Seq s(g, b);
+    const int2 r = wave_range(k < s.k_len ? g.doc[(int64_t)b * g.K + k] : -1);
+    if (threadIdx.x == 0) g.ranges[(int64_t)b * nr + e] = r;
+}
+
+// Block number -> (tile, head): the tiles of a head on one XCD (blocks reach
+// the 8 XCDs in turn), so that its L2 serves the rows they share; all heads'
+// first tiles before the second ones.
+__device__ __forceinline__ void place(int nz, int& tile, int& z) {
+    const int lid = (int)blockIdx.x;
+    if ((nz & 7) == 0) {
+        const int hp = nz >> 3, i = lid >> 3;
+        tile = i / hp;
+        z = (i - tile * hp) * 8 + (lid & 7);
+    } else {
+        tile = lid / nz;
+        z = lid - tile * nz;
+    }
+}
+
+// Score of a lane's query and one key from the raw product: in units of log2.
+template <typename T, bool CAP>
+__device__ __forceinline__ float score(float raw, float scale2, float rcap, float cap2, float slope2, int pos, int key,
+                                       float& t) {
+    float s;
+    if constexpr (CAP) {
+        t = cap_tanh<T>(raw * rcap);
+        s = t * cap2;
+    } else {
+        s = raw * scale2;
+    }
+    return fmaf(-slope2, fabsf((float)(pos - key)), s);
+}
+
+// ------------------------------------------------------------- forward
+// A block takes 32 WQ query rows; its waves lie WQ along the queries and
+// WK = 4 / WQ along the keys of a step (each wave 32 NS of them).
+template <typename T, int DP, bool CAP, int WQ, int NS>
+__global__ __launch_bounds__(NT) void fwd_k(StreamArgs g) {
+    constexpr int WK = 4 / WQ, BM = 32 * WQ, BN = 32 * WK * NS, ND = DP / 32, NC = DP / 16;
+    using TL = Tile<T, DP>;
+    constexpr int TB = BN * TL::PITCH;
+    // joining the waves along the keys: m, l and o of all but the first
+    constexpr int JOIN = WK > 1 ? (WK - 1) * 64 * (2 + 16 * ND) * 4 : 0;
+    __shared__ __attribute__((aligned(16))) char lds[(2 * TB > JOIN ? 2 * TB : JOIN) + BN * 4];
+    char *tk = lds, *tv = lds + TB;
+    int* kdoc = reinterpret_cast<int*>(lds + (2 * TB > JOIN ? 2 * TB : JOIN));
+
+    const int hz = g.H / g.pack, rows = g.J * g.pack, nqt = (rows + BM - 1) / BM;
+    int tile, z;
+    place(g.B * hz * g.splits, tile, z);
+    const int split = z % g.splits;
+    z /= g.splits;
+    if (g.causal) tile = nqt - 1 - tile;  // rows with the most keys first
+    const int b = z / hz, h0 = (z - b * hz) * g.pack, kvh = h0 / (g.H / g.G);
+    const int tid = threadIdx.x, lane = tid & 63, c32 = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wq = wave % WQ, wk = wave / WQ;
+    const Seq sq(g, b);
+
+    const int r0 = tile * BM, row = r0 + 32 * wq + c32;  // this lane's query row
+    const int j = row / g.pack, h = h0 + row - j * g.pack;
+    const bool live = row < rows && j < sq.q_len;
+    const int hi = live ? sq.hi(g, j) : 0, pos = sq.off + j;
+    const int mydoc = g.doc && live ? sq.doc_of(g, b, j) : -1;
+    const float slope2 = g.slopes && live ? g.slopes[h] * LOG2E : 0.f;
+    const float scale2 = g.scaler * LOG2E, rcap = CAP ? g.scaler / g.cap : 0.f, cap2 = g.cap * LOG2E;
+
+    Frag<T> qf[NC];
+    {
+        const T* qp = reinterpret_cast<const T*>(g.q.ptr) + b * g.q.sb + h * g.q.sh + j * g.q.st;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int e = 16 * c + 8 * hh;
+            qf[c] = live && e < g.P ? frag_load<T>(qp + e) : frag_zero<T>();
+        }
+    }
+
+    // rows of the block that hold queries: the last has the largest hi, the
+    // first of a wave the smallest
+    const int jlast = min(min(r0 + BM, rows) - 1, sq.q_len * g.pack - 1) / g.pack;
+    const int hi_all = r0 < sq.q_len * g.pack ? sq.hi(g, jlast) : 0;
+    const int wrow = r0 + 32 * wq, hi_low = wrow + 31 < sq.q_len * g.pack ? sq.hi(g, wrow / g.pack) : 0;
+    int2 qr{0, 0};
+    if (g.doc) {
+        __shared__ int2 wrange[4];
+        const int2 r = wave_range(mydoc);
+        if (lane == 0) wrange[wave] = r;
+        __syncthreads();
+        qr = wrange[0];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) qr = int2{min(qr.x, wrange[w].x), max(qr.y, wrange[w].y)};
+    }
+    const int steps = (hi_all + BN - 1) / BN, per = (steps + g.splits - 1) / g.splits;
+    const int s_end = min(steps, (split + 1) * per);
+    int s = split * per;
+    const int nr = (g.K + STREAM_RANGE - 1) / STREAM_RANGE;
+    // next step from s on whose keys may be of the rows' documents
+    auto next = [&](int from) {
+        if (!g.doc) return from;
+        for (; from < s_end; from += 64) {
+            bool in = false;
+            if (from + lane < s_end) {
+#pragma unroll
+                for (int i = 0; i < BN / STREAM_RANGE; ++i) {
+                    const int e = (from + lane) * (BN / STREAM_RANGE) + i;
+                    if (e < nr) in |= ranges_meet(g.ranges[(int64_t)b * nr + e], qr);
+                }
+            }
+            const uint64_t m = __ballot(in);
+            if (m) return from + (int)__builtin_ctzll(m);
+        }
+        return s_end;
+    };
+
+    const T* kp = reinterpret_cast<const T*>(g.k.ptr) + b * g.k.sb + kvh * g.k.sh;
+    const T* vp = reinterpret_cast<const T*>(g.v.ptr) + b * g.v.sb + kvh * g.v.sh;
+    const int32_t* docs = g.doc ? g.doc + (int64_t)b * g.K : nullptr;
+    Stage<T, DP, BN> sk, sv;
+    int sdoc = -1;
+    auto fetch = [&](int step) {
+        const int k0 = step * BN;
+        auto ok = [&](int r) { return k0 + r < sq.k_len && (!docs || docs[k0 + r] >= 0); };
+        sk.load(tid, g.P, ok, [&](int r) { return kp + (int64_t)(k0 + r) * g.k.st; });
+        sv.load(tid, g.P, ok, [&](int r) { return vp + (int64_t)(k0 + r) * g.v.st; });
+        if (docs && tid < BN) sdoc = k0 + tid < sq.k_len ? docs[k0 + tid] : -1;
+    };
+
+    floatx16 o[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    float m = -INFINITY, l = 0.f;
+
+    s = next(s);
+    if (s < s_end) fetch(s);
+    while (s < s_end) {
+        __syncthreads();
+        sk.store(tid, tk);
+        sv.store(tid, tv);
+        if (docs && tid < BN) kdoc[tid] = sdoc;
+        __syncthreads();
+        const int k0 = s * BN + 32 * NS * wk;  // this wave's keys
+        s = next(s + 1);
+        if (s < s_end) fetch(s);
+
+        float x[NS][16];
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            floatx16 acc;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                acc = mma<T>(TL::row(tk, 32 * (NS * wk + n) + c32, 16 * c + 8 * hh), qf[c], acc);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[n][i] = acc[i];
+        }
+        float t;
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                x[n][i] = score<T, CAP>(x[n][i], scale2, rcap, cap2, slope2, pos,
+                                        k0 + 32 * n + 8 * (i >> 2) + 4 * hh + (i & 3), t);
+        if (k0 + 32 * NS > hi_low || docs) {
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int kk = 32 * n + 8 * q + 4 * hh;
+                    int4 kd{mydoc, mydoc, mydoc, mydoc};
+                    if (docs) kd = *reinterpret_cast<const int4*>(kdoc + 32 * NS * wk + kk);
+                    const int id[4] = {kd.x, kd.y, kd.z, kd.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (k0 + kk + i >= hi || (docs && (id[i] != mydoc || mydoc < 0))) x[n][4 * q + i] = -INFINITY;
+                }
+        }
+        float mx = x[0][0];
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[n][i]);
+        mx = fmaxf(m, fmaxf(mx, other_half(mx)));
+        const float ms = mx == -INFINITY ? 0.f : mx;
+        const float alpha = __builtin_amdgcn_exp2f(m - ms);
+        m = mx;
+        l *= alpha;
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[n][i] = __builtin_amdgcn_exp2f(x[n][i] - ms);
+                l += x[n][i];
+            }
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const Frag<T> p = frag_acc<T>(&x[n][8 * c]);
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+                    o[d] = mma<T>(TL::col(tv, 32 * (NS * wk + n) + 16 * c, 32 * d, lane), p, o[d]);
+            }
+    }
+    l += other_half(l);
+
+    if constexpr (WK > 1) {
+        // join the waves along the keys, in wave order
+        __syncthreads();
+        float* jm = reinterpret_cast<float*>(lds);
+        if (wk > 0) {
+            float* w = jm + (wk - 1) * 64 * (2 + 16 * ND) + lane;
+            w[0] = m;
+            w[64] = l;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[64 * (2 + 16 * d + i)] = o[d][i];
+        }
+        __syncthreads();
+        if (wk > 0) return;
+#pragma unroll
+        for (int w = 0; w < WK - 1; ++w) {
+            const float* p = jm + w * 64 * (2 + 16 * ND) + lane;
+            const float mn = fmaxf(m, p[0]), ms = mn == -INFINITY ? 0.f : mn;
+            const float a = __builtin_amdgcn_exp2f(m - ms), c = __builtin_amdgcn_exp2f(p[0] - ms);
+            m = mn;
+            l = l * a + p[64] * c;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * a + p[64 * (2 + 16 * d + i)] * c;
+        }
+    }
+    if (row >= rows) return;
+    const int64_t zr = ((int64_t)b * g.H + h) * g.J + j;
+    if (g.splits > 1) {
+        const int64_t at = (int64_t)split * g.B * g.H * g.J + zr;
+        if (hh == 0) g.part_ml[at] = float2{m, l};
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int e = 32 * d + 8 * q + 4 * hh;
+                if (e < g.P)
+                    *reinterpret_cast<floatx4*>(g.part_o + at * g.P + e) =
+                        floatx4{o[d][4 * q], o[d][4 * q + 1], o[d][4 * q + 2], o[d][4 * q + 3]};
+            }
+        return;
+    }
+    // (a row that sees no key: zeros, and +inf so that 2^(s - lse) is zero)
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    if (g.lse && hh == 0) g.lse[zr] = l > 0.f ? m + __builtin_amdgcn_logf(l) : INFINITY;
+    T* op = reinterpret_cast<T*>(g.o.ptr) + b * g.o.sb + h * g.o.sh + j * g.o.st;
+    T* lp = g.lo ? reinterpret_cast<T*>(g.lo) + (((int64_t)b * g.J + j) * g.H + h) * g.P : nullptr;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int e = 32 * d + 8 * q + 4 * hh;
+            if (e >= g.P) continue;
+            float y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = o[d][4 * q + i] * inv;
+            store4<T>(op + e, y);
+            if (lp) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] -= to_f(from_f<T>(y[i]));
+                store4<T>(lp + e, y);
+            }
+        }
+}
+
+// Joins the parts that fwd_k left, in their order: 16 lanes a row.
+template <typename T>
+__global__ __launch_bounds__(NT) void join_k(StreamArgs g) {
+    const int64_t n = (int64_t)g.B * g.H * g.J, zr = ((int64_t)blockIdx.x * NT + threadIdx.x) >> 4;
+    const int gl = threadIdx.x & 15;
+    if (zr >= n) return;
+    const int j = (int)(zr % g.J), h = (int)(zr / g.J % g.H), b = (int)(zr / g.J / g.H);
+    float m = -INFINITY;
+    for (int s = 0; s < g.splits; ++s) m = fmaxf(m, g.part_ml[s * n + zr].x);
+    const float ms = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    for (int s = 0; s < g.splits; ++s) {
+        const float2 p = g.part_ml[s * n + zr];
+        l += p.y * __builtin_amdgcn_exp2f(p.x - ms);
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    if (g.lse && gl == 0) g.lse[zr] = l > 0.f ? m + __builtin_amdgcn_logf(l) : INFINITY;
+    T* op = reinterpret_cast<T*>(g.o.ptr) + b * g.o.sb + h * g.o.sh + j * g.o.st;
+    T* lp = g.lo ? reinterpret_cast<T*>(g.lo) + (((int64_t)b * g.J + j) * g.H + h) * g.P : nullptr;
+    for (int e = 8 * gl; e < g.P; e += 128) {
+        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < g.splits; ++s) {
+            const float w = __builtin_amdgcn_exp2f(g.part_ml[s * n + zr].x - ms) * inv;
+            float x[8];
+            V8<float>::load(g.part_o + (s * n + zr) * g.P + e, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = fmaf(w, x[i], y[i]);
+        }
+        V8<T>::store(op + e, y);
+        if (lp) {
+            float lo[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) lo[i] = y[i] - to_f(from_f<T>(y[i]));
+            V8<T>::store(lp + e, lo);
+        }
+    }
+}
+
+// ------------------------------------------------------------ backward
+// Row terms D = dout . out, out as the forward had it before rounding (its
+// stored value and the saved rest): 16 lanes a row, 16 rows a step of a
+// block.  fp16 also: the largest |dout| of every 256 rows of a head, from
+// which the score gradients get a power of two that keeps them out of the
+// type's subnormal numbers (a probability of 1e-5 times a small gradient
+// would lose its bits there).
+template <typename T>
+__global__ __launch_bounds__(NT) void rows_k(StreamArgs g) {
+    const int nch = (g.J + STREAM_DROWS - 1) / STREAM_DROWS, z = (int)blockIdx.x / nch, ch = (int)blockIdx.x - z * nch;
+    const int b = z / g.H, h = z - b * g.H, gl = threadIdx.x & 15;
+    const Seq s(g, b);
+    float top = 0.f;
+    for (int r = threadIdx.x >> 4; r < STREAM_DROWS; r += NT / 16) {
+        const int j = ch * STREAM_DROWS + r;
+        if (j >= g.J) break;
+        float d = 0.f;
+        const bool in = j < s.q_len && !(g.doc && s.doc_of(g, b, j) < 0);
+        if (in && 8 * gl < g.P) {
+            float a[8], y[8];
+            V8<T>::load(reinterpret_cast<const T*>(g.dout.ptr) + b * g.dout.sb + h * g.dout.sh + j * g.dout.st + 8 * gl, a);
+            V8<T>::load(reinterpret_cast<const T*>(g.o.ptr) + b * g.o.sb + h * g.o.sh + j * g.o.st + 8 * gl, y);
+            if constexpr (sizeof(T) == 2) {
+                float lo[8];
+                V8<T>::load(reinterpret_cast<const T*>(g.lo) + (((int64_t)b * g.J + j) * g.H + h) * g.P + 8 * gl, lo);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] += lo[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                d = fmaf(a[i], y[i], d);
+                top = fmaxf(top, fabsf(a[i]));
+            }
+        }
+        d = group_sum<16>(d);
+        if (gl == 0) g.dsum[(int64_t)z * g.J + j] = d;
+    }
+    if (g.dmax) {
+        __shared__ float w[NT / 64];
+        top = group_max<64>(top);
+        if ((threadIdx.x & 63) == 0) w[threadIdx.x >> 6] = top;
+        __syncthreads();
+        if (threadIdx.x == 0) g.dmax[(int64_t)z * g.dmax_n + ch] = fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
+    }
+}
+
+// fp16: probabilities are held as 2^10 p; score gradients as 2^e ds with
+// 2^e about 1 / max |dout| over the heads of a key/value head, so that they
+// are at most about 2 p sum |v| and keep all their bits down to 6e-5 of
+// that scale; what would pass the type's largest value is held to it.
+struct Gain {
+    float p2;   // added to the exponents of the probabilities
+    float pinv; // 1 / 2^p2
+    float ds, dsinv;  // (dout . v - D) times ds; 1 / (ds 2^p2)
+};
+template <typename T>
+__device__ __forceinline__ Gain gain(const StreamArgs& g, int b, int kvh) {
+    if constexpr (!__is_same(T, half_t)) return Gain{0.f, 1.f, 1.f, 1.f};
+    const int n = g.H / g.G * g.dmax_n;
+    const float* p = g.dmax + ((int64_t)b * g.H + kvh * (g.H / g.G)) * g.dmax_n;
+    float top = 0.f;
+    for (int i = threadIdx.x & 63; i < n; i += 64) top = fmaxf(top, p[i]);
+    top = group_max<64>(top);
+    const int e = top > 0.f && top < INFINITY ? -ilogbf(top) : 0;
+    return Gain{10.f, 1.f / 1024.f, ldexpf(1.f, e - 10), ldexpf(1.f, -e)};
+}
+template <typename T> __device__ __forceinline__ float held(float x) {
+    if constexpr (__is_same(T, half_t)) return x > 65504.f ? 65504.f : x < -65504.f ? -65504.f : x;  // (NaN stays)
+    return x;
+}
+
+// dK and dV of 128 keys (32 a wave) of one key/value head: walks the query
+// rows of all its query heads, 64 a step.
+template <typename T, int DP, bool CAP>
+__global__ __launch_bounds__(NT) void dkv_k(StreamArgs g) {
+    constexpr int BQ = 64, ND = DP / 32, NC = DP / 16;
+    using TL = Tile<T, DP>;
+    constexpr int TB = BQ * TL::PITCH;
+    __shared__ __attribute__((aligned(16))) char lds[2 * TB];
+    __shared__ __attribute__((aligned(16))) float row_lse[BQ], row_d[BQ];
+    __shared__ __attribute__((aligned(16))) int row_hi[BQ], row_doc[BQ];
+    char *tq = lds, *td = lds + TB;
+    int tile, z;
+    place(g.B * g.G, tile, z);
+    const int b = z / g.G, kvh = z - b * g.G, grp = g.H / g.G, k0 = tile * STREAM_KEYS;
+    const int tid = threadIdx.x, lane = tid & 63, c32 = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Seq sq(g, b);
+    const int32_t* docs = g.doc ? g.doc + (int64_t)b * g.K : nullptr;
+    const int key = k0 + 32 * wave + c32;
+    const int kd = docs ? (key < sq.k_len ? docs[key] : -1) : 0;
+    const bool kin = key < sq.k_len && kd >= 0;
+    const float scale2 = g.scaler * LOG2E, rcap = CAP ? g.scaler / g.cap : 0.f, cap2 = g.cap * LOG2E;
+    const Gain gn = gain<T>(g, b, kvh);
+
+    Frag<T> kf[NC], vf[NC];
+    {
+        const T* kp = reinterpret_cast<const T*>(g.k.ptr) + b * g.k.sb + kvh * g.k.sh + (int64_t)key * g.k.st;
+        const T* vp = reinterpret_cast<const T*>(g.v.ptr) + b * g.v.sb + kvh * g.v.sh + (int64_t)key * g.v.st;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int e = 16 * c + 8 * hh;
+            kf[c] = kin && e < g.P ? frag_load<T>(kp + e) : frag_zero<T>();
+            vf[c] = kin && e < g.P ? frag_load<T>(vp + e) : frag_zero<T>();
+        }
+    }
+    floatx16 dk[ND], dv[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.f;
+
+    // query steps that may see one of these keys: rows from the first whose
+    // position reaches them, all where the prefix does
+    const int first = g.causal && sq.prefix <= k0 ? max(0, k0 - sq.off) / BQ : 0;
+    const int nst = k0 < sq.k_len ? (sq.q_len + BQ - 1) / BQ : 0;
+    const int nr = (g.K + STREAM_RANGE - 1) / STREAM_RANGE;
+    int2 kr{0, 0};
+    if (docs) {
+        kr = int2{INT32_MAX, -1};
+#pragma unroll
+        for (int i = 0; i < STREAM_KEYS / STREAM_RANGE; ++i) {
+            const int e = k0 / STREAM_RANGE + i;
+            if (e < nr) {
+                const int2 r = g.ranges[(int64_t)b * nr + e];
+                kr = int2{min(kr.x, r.x), max(kr.y, r.y)};
+            }
+        }
+    }
+    auto next = [&](int from) {
+        if (!docs) return from;
+        for (; from < nst; from += 64) {
+            bool in = false;
+            if (from + lane < nst) {
+                // the step's rows lie in at most two entries
+                const int p = sq.off + (from + lane) * BQ, e0 = max(p, 0) / STREAM_RANGE;
+                const int e1 = max(p + BQ - 1, 0) / STREAM_RANGE;
+                if (e0 < nr) in |= ranges_meet(g.ranges[(int64_t)b * nr + e0], kr);
+                if (e1 < nr) in |= ranges_meet(g.ranges[(int64_t)b * nr + e1], kr);
+            }
+            const uint64_t mk = __ballot(in);
+            if (mk) return from + (int)__builtin_ctzll(mk);
+        }
+        return nst;
+    };
+
+    for (int hg = 0; hg < grp; ++hg) {
+        const int h = kvh * grp + hg;
+        const float slope2 = g.slopes ? g.slopes[h] * LOG2E : 0.f;
+        const T* qp = reinterpret_cast<const T*>(g.q.ptr) + b * g.q.sb + h * g.q.sh;
+        const T* dp = reinterpret_cast<const T*>(g.dout.ptr) + b * g.dout.sb + h * g.dout.sh;
+        const int64_t zr = ((int64_t)b * g.H + h) * g.J;
+        Stage<T, DP, BQ> st_q, st_d;
+        float f_lse = INFINITY, f_d = 0.f;
+        int f_hi = 0, f_doc = -1;
+        auto fetch = [&](int step) {
+            const int j0 = step * BQ;
+            auto ok = [&](int r) { return j0 + r < sq.q_len && (!docs || sq.doc_of(g, b, j0 + r) >= 0); };
+            st_q.load(tid, g.P, ok, [&](int r) { return qp + (int64_t)(j0 + r) * g.q.st; });
+            st_d.load(tid, g.P, ok, [&](int r) { return dp + (int64_t)(j0 + r) * g.dout.st; });
+            if (tid < BQ) {
+                const int j = j0 + tid;
+                const bool in = j < sq.q_len;
+                f_lse = in ? g.lse[zr + j] : INFINITY;
+                f_d = in ? g.dsum[zr + j] : 0.f;
+                f_hi = sq.hi(g, j);
+                f_doc = docs ? sq.doc_of(g, b, j) : 0;
+            }
+        };
+        int s = next(first);
+        if (s < nst) fetch(s);
+        while (s < nst) {
+            __syncthreads();
+            st_q.store(tid, tq);
+            st_d.store(tid, td);
+            if (tid < BQ) {
+                row_lse[tid] = f_lse - gn.p2;
+                row_d[tid] = f_d;
+                row_hi[tid] = f_hi;
+                row_doc[tid] = f_doc;
+            }
+            __syncthreads();
+            const int j0 = s * BQ;
+            s = next(s + 1);
+            if (s < nst) fetch(s);
+
+#pragma unroll
+            for (int n = 0; n < BQ / 32; ++n) {
+                floatx16 sc, dpv;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[i] = dpv[i] = 0.f;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    sc = mma<T>(TL::row(tq, 32 * n + c32, 16 * c + 8 * hh), kf[c], sc);
+                    dpv = mma<T>(TL::row(td, 32 * n + c32, 16 * c + 8 * hh), vf[c], dpv);
+                }
+                float p[16], ds[16];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int r = 32 * n + 8 * q + 4 * hh;
+                    const floatx4 ls = *reinterpret_cast<const floatx4*>(row_lse + r);
+                    const floatx4 dd = *reinterpret_cast<const floatx4*>(row_d + r);
+                    const int4 rh = *reinterpret_cast<const int4*>(row_hi + r);
+                    const int4 rd = *reinterpret_cast<const int4*>(row_doc + r);
+                    const int hi4[4] = {rh.x, rh.y, rh.z, rh.w}, id4[4] = {rd.x, rd.y, rd.z, rd.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int a = 4 * q + i;
+                        float t = 0.f;
+                        const float x = score<T, CAP>(sc[a], scale2, rcap, cap2, slope2, sq.off + j0 + r + i, key, t);
+                        const bool see = key < hi4[i] && kin && id4[i] == kd;
+                        p[a] = see ? __builtin_amdgcn_exp2f(x - ls[i]) : 0.f;
+                        float y = p[a] * (dpv[a] - dd[i]) * gn.ds;
+                        if constexpr (CAP) y *= 1.f - t * t;
+                        ds[a] = see ? held<T>(y) : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const Frag<T> pf = frag_acc<T>(p + 8 * c), sf = frag_acc<T>(ds + 8 * c);
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        dv[d] = mma<T>(TL::col(td, 32 * n + 16 * c, 32 * d, lane), pf, dv[d]);
+                        dk[d] = mma<T>(TL::col(tq, 32 * n + 16 * c, 32 * d, lane), sf, dk[d]);
+                    }
+                }
+            }
+        }
+    }
+    if (key >= g.K) return;
+    T* dkp = reinterpret_cast<T*>(g.dk.ptr) + b * g.dk.sb + kvh * g.dk.sh + (int64_t)key * g.dk.st;
+    T* dvp = reinterpret_cast<T*>(g.dv.ptr) + b * g.dv.sb + kvh * g.dv.sh + (int64_t)key * g.dv.st;
+    const float fk = g.scaler * gn.dsinv;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int e = 32 * d + 8 * q + 4 * hh;
+            if (e >= g.P) continue;
+            float y[4], w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                y[i] = dk[d][4 * q + i] * fk;
+                w[i] = dv[d][4 * q + i] * gn.pinv;
+            }
+            store4<T>(dkp + e, y);
+            store4<T>(dvp + e, w);
+        }
+}
+
+// dQ of 128 query rows (32 a wave) of one head: walks their keys as the
+// forward does.
+template <typename T, int DP, bool CAP>
+__global__ __launch_bounds__(NT) void dq_k(StreamArgs g) {
+    constexpr int BM = 128, BN = 64, NS = 2, ND = DP / 32, NC = DP / 16;
+    using TL = Tile<T, DP>;
+    constexpr int TB = BN * TL::PITCH;
+    __shared__ __attribute__((aligned(16))) char lds[2 * TB];
+    __shared__ __attribute__((aligned(16))) int kdoc[BN];
+    __shared__ int2 wrange[4];
+    char *tk = lds, *tv = lds + TB;
+    const int nqt = (g.J + BM - 1) / BM;
+    int tile, z;
+    place(g.B * g.H, tile, z);
+    if (g.causal) tile = nqt - 1 - tile;
+    const int b = z / g.H, h = z - b * g.H, kvh = h / (g.H / g.G);
+    const int tid = threadIdx.x, lane = tid & 63, c32 = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Seq sq(g, b);
+    const int j0 = tile * BM, j = j0 + 32 * wave + c32, pos = sq.off + j;
+    const int32_t* docs = g.doc ? g.doc + (int64_t)b * g.K : nullptr;
+    const int mydoc = docs ? sq.doc_of(g, b, j) : 0;
+    const bool live = j < sq.q_len && mydoc >= 0;
+    const int hi = live ? sq.hi(g, j) : 0;
+    const float slope2 = g.slopes ? g.slopes[h] * LOG2E : 0.f;
+    const float scale2 = g.scaler * LOG2E, rcap = CAP ? g.scaler / g.cap : 0.f, cap2 = g.cap * LOG2E;
+    const Gain gn = gain<T>(g, b, kvh);
+    const int64_t zr = ((int64_t)b * g.H + h) * g.J + j;
+    const float lse = live ? g.lse[zr] - gn.p2 : INFINITY, dd = live ? g.dsum[zr] : 0.f;
+
+    Frag<T> qf[NC], df[NC];
+    {
+        const T* qp = reinterpret_cast<const T*>(g.q.ptr) + b * g.q.sb + h * g.q.sh + (int64_t)j * g.q.st;
+        const T* dp = reinterpret_cast<const T*>(g.dout.ptr) + b * g.dout.sb + h * g.dout.sh + (int64_t)j * g.dout.st;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int e = 16 * c + 8 * hh;
+            qf[c] = live && e < g.P ? frag_load<T>(qp + e) : frag_zero<T>();
+            df[c] = live && e < g.P ? frag_load<T>(dp + e) : frag_zero<T>();
+        }
+    }
+    const int jlast = min(min(j0 + BM, g.J), sq.q_len) - 1;
+    const int steps = j0 < sq.q_len ? (sq.hi(g, jlast) + BN - 1) / BN : 0;
+    int2 qr{0, 0};
+    if (docs) {
+        const int2 r = wave_range(mydoc);
+        if (lane == 0) wrange[wave] = r;
+        __syncthreads();
+        qr = wrange[0];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) qr = int2{min(qr.x, wrange[w].x), max(qr.y, wrange[w].y)};
+    }
+    const int nr = (g.K + STREAM_RANGE - 1) / STREAM_RANGE;
+    auto next = [&](int from) {
+        if (!docs) return from;
+        for (; from < steps; from += 64) {
+            const bool in = from + lane < steps && ranges_meet(g.ranges[(int64_t)b * nr + from + lane], qr);
+            const uint64_t mk = __ballot(in);
+            if (mk) return from + (int)__builtin_ctzll(mk);
+        }
+        return steps;
+    };
+    const T* kp = reinterpret_cast<const T*>(g.k.ptr) + b * g.k.sb + kvh * g.k.sh;
+    const T* vp = reinterpret_cast<const T*>(g.v.ptr) + b * g.v.sb + kvh * g.v.sh;
+    Stage<T, DP, BN> sk, sv;
+    int sdoc = -1;
+    auto fetch = [&](int step) {
+        const int k0 = step * BN;
+        auto ok = [&](int r) { return k0 + r < sq.k_len && (!docs || docs[k0 + r] >= 0); };
+        sk.load(tid, g.P, ok, [&](int r) { return kp + (int64_t)(k0 + r) * g.k.st; });
+        sv.load(tid, g.P, ok, [&](int r) { return vp + (int64_t)(k0 + r) * g.v.st; });
+        if (docs && tid < BN) sdoc = k0 + tid < sq.k_len ? docs[k0 + tid] : -1;
+    };
+    floatx16 dq[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dq[d][i] = 0.f;
+
+    int s = next(0);
+    if (s < steps) fetch(s);
+    while (s < steps) {
+        __syncthreads();
+        sk.store(tid, tk);
+        sv.store(tid, tv);
+        if (docs && tid < BN) kdoc[tid] = sdoc;
+        __syncthreads();
+        const int k0 = s * BN;
+        s = next(s + 1);
+        if (s < steps) fetch(s);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            floatx16 sc, dpv;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[i] = dpv[i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                sc = mma<T>(TL::row(tk, 32 * n + c32, 16 * c + 8 * hh), qf[c], sc);
+                dpv = mma<T>(TL::row(tv, 32 * n + c32, 16 * c + 8 * hh), df[c], dpv);
+            }
+            float ds[16];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int kk = 32 * n + 8 * q + 4 * hh;
+                int4 kd{mydoc, mydoc, mydoc, mydoc};
+                if (docs) kd = *reinterpret_cast<const int4*>(kdoc + kk);
+                const int id[4] = {kd.x, kd.y, kd.z, kd.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int a = 4 * q + i;
+                    float t = 0.f;
+                    const float x = score<T, CAP>(sc[a], scale2, rcap, cap2, slope2, pos, k0 + kk + i, t);
+                    const bool see = k0 + kk + i < hi && id[i] == mydoc;
+                    float y = __builtin_amdgcn_exp2f(x - lse) * (dpv[a] - dd) * gn.ds;
+                    if constexpr (CAP) y *= 1.f - t * t;
+                    ds[a] = see ? held<T>(y) : 0.f;
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const Frag<T> sf = frag_acc<T>(ds + 8 * c);
+#pragma unroll
+                for (int d = 0; d < ND; ++d) dq[d] = mma<T>(TL::col(tk, 32 * n + 16 * c, 32 * d, lane), sf, dq[d]);
+            }
+        }
+    }
+    if (j >= g.J) return;
+    T* dqp = reinterpret_cast<T*>(g.dq.ptr) + b * g.dq.sb + h * g.dq.sh + (int64_t)j * g.dq.st;
+    const float f = g.scaler * gn.dsinv;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int e = 32 * d + 8 * q + 4 * hh;
+            if (e >= g.P) continue;
+            float y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = dq[d][4 * q + i] * f;
+            store4<T>(dqp + e, y);
+        }
+}
+
+// ------------------------------------------------------------- launches
+template <typename T, int DP, bool CAP> void launch_fwd(const StreamArgs& a, bool few, hipStream_t st) {
+    const int64_t rows = (int64_t)a.J * a.pack, nz = (int64_t)a.B * (a.H / a.pack) * a.splits;
+    if (few)
+        fwd_k<T, DP, CAP, 1, 1><<<dim3((unsigned)((rows + 31) / 32 * nz)), NT, 0, st>>>(a);
+    else
+        fwd_k<T, DP, CAP, 4, 2><<<dim3((unsigned)((rows + STREAM_BM - 1) / STREAM_BM * nz)), NT, 0, st>>>(a);
+}
+
+template <typename T, int DP, bool CAP> void launch_bwd(const StreamArgs& a, hipStream_t st) {
+    const int64_t nk = (int64_t)((a.K + STREAM_KEYS - 1) / STREAM_KEYS) * a.B * a.G;
+    const int64_t nq = (int64_t)((a.J + 127) / 128) * a.B * a.H;
+    if (nk > 0) dkv_k<T, DP, CAP><<<dim3((unsigned)nk), NT, 0, st>>>(a);
+    if (nq > 0) dq_k<T, DP, CAP><<<dim3((unsigned)nq), NT, 0, st>>>(a);
+}
+
+}  // namespace stream
+
+#define DM_STREAM_PICK(FN, ...)                                         \
+    do {                                                                \
+        const int dp_ = stream_head_pad(a.P);                           \
+        if (a.cap > 0.f) {                                              \
+            if (dp_ == 32) stream::FN<T, 32, true>(__VA_ARGS__);        \
+            else if (dp_ == 64) stream::FN<T, 64, true>(__VA_ARGS__);   \
+            else stream::FN<T, 128, true>(__VA_ARGS__);                 \
+        } else {                                                        \
+            if (dp_ == 32) stream::FN<T, 32, false>(__VA_ARGS__);       \
+            else if (dp_ == 64) stream::FN<T, 64, false>(__VA_ARGS__);  \
+            else stream::FN<T, 128, false>(__VA_ARGS__);                \
+        }                                                               \
+    } while (0)
+
+// (a launch without blocks is an error: what has no rows or keys is left out)
+inline int64_t stream_ranges_n(const StreamArgs& a) {
+    return (int64_t)((a.K + STREAM_RANGE - 1) / STREAM_RANGE) * a.B;
+}
+
+template <typename T> void stream_fwd(const StreamArgs& a, bool few, hipStream_t st) {
+    if (a.doc && a.K > 0) stream::ranges_k<T><<<dim3((unsigned)stream_ranges_n(a)), 64, 0, st>>>(a);
+    DM_STREAM_PICK(launch_fwd, a, few, st);
+    if (a.splits > 1) {
+        const int64_t lanes = (int64_t)a.B * a.H * a.J * 16;
+        stream::join_k<T><<<dim3((unsigned)((lanes + stream::NT - 1) / stream::NT)), stream::NT, 0, st>>>(a);
+    }
+}
+
+template <typename T> void stream_bwd(const StreamArgs& a, hipStream_t st) {
+    if (a.doc && a.K > 0) stream::ranges_k<T><<<dim3((unsigned)stream_ranges_n(a)), 64, 0, st>>>(a);
+    if (a.J > 0) {
+        const int64_t n = (int64_t)((a.J + STREAM_DROWS - 1) / STREAM_DROWS) * a.B * a.H;
+        stream::rows_k<T><<<dim3((unsigned)n), stream::NT, 0, st>>>(a);
+    }
+    DM_STREAM_PICK(launch_bwd, a, st);
+}
+
+}  // namespace dm

@@ -47,6 +47,7 @@ EXPORTED = [
     "dropout_mask", "saved_tensor_view", "attn_backward_form", "contract", "dm_last_error",
     "dm_trace_enable", "dm_trace_count", "dm_trace_get",
     "plan_create", "plan_destroy", "plan_log", "plan_log_read",
+    "attn_sizes", "attn_fwd", "attn_bwd", "embed_ws_bytes", "embed_fwd", "embed_bwd", "adamw_step",
 ]
 
 
@@ -102,6 +103,31 @@ class Dropout(C.Structure):
     _fields_ = [("p", C.c_float), ("site", C.c_uint32), ("layer", C.c_uint32), ("seed", C.c_uint64)]
 
 
+class AttnStride(C.Structure):
+    """Element strides between sequences, heads and tokens."""
+    _fields_ = [("b", C.c_int64), ("h", C.c_int64), ("t", C.c_int64)]
+
+
+class AttnDesc(C.Structure):
+    _fields_ = [("B", C.c_int32), ("J", C.c_int32), ("K", C.c_int32), ("H", C.c_int32), ("G", C.c_int32),
+                ("P", C.c_int32), ("dtype", C.c_int32), ("scaler", C.c_float), ("cap", C.c_float),
+                ("causal", C.c_int32), ("q", AttnStride), ("k", AttnStride), ("v", AttnStride), ("out", AttnStride),
+                ("q_len", C.c_void_p), ("k_len", C.c_void_p), ("doc", C.c_void_p), ("prefix", C.c_void_p),
+                ("slopes", C.c_void_p)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("master", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p),
+                ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n", C.c_int64),
+                ("decay", C.c_double)]
+
+
+class AdamwDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("state_bits", C.c_int32), ("lr", C.c_double), ("beta1", C.c_double),
+                ("beta2", C.c_double), ("eps", C.c_double), ("grad_scale", C.c_double), ("step", C.c_int64),
+                ("scalars", C.c_void_p)]
+
+
 def _sig(name, res, *args):
     f = getattr(_lib, name)
     f.restype = res
@@ -145,6 +171,14 @@ _f["dm_trace_enable"] = _sig("dm_trace_enable", I32, I32)
 _f["dm_trace_count"] = _sig("dm_trace_count", I32)
 _f["dm_trace_get"] = _sig("dm_trace_get", I32, I32, C.POINTER(C.c_char_p), C.POINTER(C.c_char_p),
                           C.POINTER(C.c_float))
+PATTN = C.POINTER(AttnDesc)
+_f["attn_sizes"] = _sig("attn_sizes", I32, PATTN, PSZ, PSZ, PSZ)
+_f["attn_fwd"] = _sig("attn_fwd", I32, PATTN, P_, P_, P_, P_, P_, P_, SZ, P_)
+_f["attn_bwd"] = _sig("attn_bwd", I32, PATTN, P_, P_, P_, P_, P_, P_, P_, P_, P_, P_, SZ, P_)
+_f["embed_ws_bytes"] = _sig("embed_ws_bytes", SZ, I64, I32, I32)
+_f["embed_fwd"] = _sig("embed_fwd", I32, I32, I64, I32, I32, P_, P_, F32, P_, P_)
+_f["embed_bwd"] = _sig("embed_bwd", I32, I32, I64, I32, I32, P_, I32, P_, F32, P_, P_, SZ, P_)
+_f["adamw_step"] = _sig("adamw_step", I32, C.POINTER(AdamwDesc), C.POINTER(AdamwTensor), I32, P_)
 _f["plan_create"] = _sig("plan_create", I32, C.POINTER(ContractChoice), I32, I32, C.POINTER(LayoutChoice),
                          C.POINTER(C.c_void_p))
 _f["plan_destroy"] = _sig("plan_destroy", I32, C.c_void_p)
@@ -336,6 +370,40 @@ def contract(dtype, batch, M, N, K, alpha, A, a_trans, sa, B, b_trans, sb, bias,
              tile_cfg=-1, splits=0, ws=None, ws_bytes=0, stream=None):
     return _call("contract", dtype, batch, M, N, K, alpha, ptr(A), a_trans, sa, ptr(B), b_trans, sb, ptr(bias),
                  ptr(Cout), out_f32, sc, tile_cfg, splits, ptr(ws), ws_bytes, _st(stream))
+
+
+# ------------------------------------- attention, embedding, optimiser step
+def attn_sizes(desc: AttnDesc):
+    s, f, b = C.c_size_t(), C.c_size_t(), C.c_size_t()
+    _call("attn_sizes", C.byref(desc), C.byref(s), C.byref(f), C.byref(b))
+    return s.value, f.value, b.value
+
+
+def attn_fwd(desc: AttnDesc, q, k, v, out, saved, ws, ws_bytes, stream=None):
+    return _call("attn_fwd", C.byref(desc), ptr(q), ptr(k), ptr(v), ptr(out), ptr(saved), ptr(ws), ws_bytes, _st(stream))
+
+
+def attn_bwd(desc: AttnDesc, q, k, v, out, saved, dout, dq, dk, dv, ws, ws_bytes, stream=None):
+    return _call("attn_bwd", C.byref(desc), ptr(q), ptr(k), ptr(v), ptr(out), ptr(saved), ptr(dout), ptr(dq), ptr(dk),
+                 ptr(dv), ptr(ws), ws_bytes, _st(stream))
+
+
+def embed_ws_bytes(tokens: int, vocab: int, cols: int) -> int:
+    return _f["embed_ws_bytes"](tokens, vocab, cols)
+
+
+def embed_fwd(dtype, tokens, vocab, cols, ids, table, scale, y, stream=None):
+    return _call("embed_fwd", dtype, tokens, vocab, cols, ptr(ids), ptr(table), scale, ptr(y), _st(stream))
+
+
+def embed_bwd(dtype, tokens, vocab, cols, ids, pad_id, dy, scale, dtable, ws, ws_bytes, stream=None):
+    return _call("embed_bwd", dtype, tokens, vocab, cols, ptr(ids), pad_id, ptr(dy), scale, ptr(dtable), ptr(ws),
+                 ws_bytes, _st(stream))
+
+
+def adamw_step(desc: AdamwDesc, tensors, count, stream=None):
+    """tensors: a ctypes array of AdamwTensor."""
+    return _call("adamw_step", C.byref(desc), tensors, count, _st(stream))
 
 
 def dm_trace_enable(on: bool) -> None:
