@@ -329,7 +329,8 @@ int attn_bwd(const dm_attn_desc* d, const void* q, const void* k, const void* v,
 
 /* ------------------------------------------------- embedding
  * y[t] = scale * table[ids[t]] over tokens x cols (table [vocab][cols]; ids
- * device int32).  An id outside 0 .. vocab-1 gives zeros.  cols up to 16384. */
+ * device int32).  An id outside 0 .. vocab-1 gives zeros.  cols up to 16384,
+ * tokens up to 2^30. */
 int embed_fwd(int32_t dtype, int64_t tokens, int32_t vocab, int32_t cols, const int32_t* ids,
               const void* table, float scale, void* y, void* stream);
 

@@ -1,4 +1,6 @@
 // Embedding lookup and its gradient.
+#include <algorithm>
+
 #include "checks.hpp"
 
 namespace dm {
@@ -27,53 +29,383 @@ __global__ __launch_bounds__(NT) void embed_fwd_k(int64_t tokens, int vocab, int
     }
 }
 
-// dtable rows of a block: it looks through all ids for those of its rows
-// and adds up their tokens' gradients, in the order of the tokens, in LDS.
-constexpr int EROWS = 16, ECOLS = 1024;
-template <typename T>
-__global__ __launch_bounds__(NT) void embed_bwd_k(int64_t tokens, int vocab, int cols, const int32_t* ids, int pad,
-                                                  const T* dy, float scale, float* dtable) {
-    __shared__ float acc[EROWS * ECOLS];
-    __shared__ int hit_t[NT], hit_r[NT];
-    __shared__ int wcount[NT / 64];
-    const int v0 = (int)blockIdx.x * EROWS, c0 = (int)blockIdx.y * ECOLS, nc = min(ECOLS, cols - c0);
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    for (int i = tid; i < EROWS * ECOLS; i += NT) acc[i] = 0.f;
-    __syncthreads();
-    for (int64_t t0 = 0; t0 < tokens; t0 += NT) {
-        const int64_t t = t0 + tid;
-        const int id = t < tokens ? ids[t] : -1;
-        const bool hit = id >= v0 && id < v0 + EROWS && id < vocab && id != pad;
-        const uint64_t m = __ballot(hit);
-        if (lane == 0) wcount[wave] = __popcll(m);
-        __syncthreads();
-        int at = 0, n = 0;
+// ------------------------------------------------------------ gradient
+// dtable[v] = scale sum over the tokens of id v: the tokens are sorted by id
+// (stable: the order of the sums is given by the ids alone), then every
+// wave adds up 32 neighbours of the sorted list, writing the rows whose
+// tokens all lie there and leaving partial sums of the first and the last
+// otherwise, which a last pass joins in order.  So the work is even however
+// often an id occurs, dy is read once, and rows that no token has come from
+// the fill that runs beside the sort: the pass is bound by writing dtable
+// and reading dy.
+//
+// Up to 16384 tokens are sorted by one block in LDS while the other blocks
+// fill; more by passes over blocks of tokens (count, scan, place).
+constexpr int PIECE = 32;          // sorted tokens of a wave
+constexpr int RUN_TOKENS = 1024;   // up to here a wave follows its last id to the end instead of leaving it in parts:
+                                   // one launch less where launches are what counts
+constexpr int SORT_TOKENS = 16384;
+constexpr int IDX_BITS = 14;       // of a token's number in the one-block sort, below its id
+constexpr int SORT_NT = 1024, SORT_W = SORT_NT / 64;
+constexpr int BINS = 256;          // of a pass: 8 bits
+constexpr int PASS_NT = 256, PASS_W = PASS_NT / 64;
+constexpr int PASS_BLOCKS = 1024;
+
+// An id as a sorting key: ids outside the table and the padding id come last.
+__device__ __forceinline__ uint32_t key_of(int id, int vocab, int pad) {
+    return id >= 0 && id < vocab && id != pad ? (uint32_t)id : (uint32_t)vocab;
+}
+
+// Lanes of the wave with the same digit, among the `in` lanes.
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, bool in) {
+    uint64_t m = __ballot(in);
 #pragma unroll
-        for (int w = 0; w < NT / 64; ++w) {
-            if (w < wave) at += wcount[w];
-            n += wcount[w];
+    for (int b = 0; b < 8; ++b) {
+        const uint64_t s = __ballot((d >> b) & 1u);
+        m &= (d >> b) & 1u ? s : ~s;
+    }
+    return m;
+}
+
+// Exclusive sums of x[0 .. n) in LDS, in place; n a multiple of 4 * NT.
+template <int THREADS> __device__ void scan_lds(uint32_t* x, int n, uint32_t* wsum) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    uint32_t carry = 0;
+    for (int i0 = 0; i0 < n; i0 += 4 * THREADS) {
+        uint32_t v[4], t = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[k] = x[i0 + 4 * tid + k];
+            t += v[k];
         }
-        if (hit) {
-            at += __popcll(m & ((1ull << lane) - 1));
-            hit_t[at] = tid;
-            hit_r[at] = id - v0;
+        uint32_t inc = t;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const uint32_t o = __shfl_up(inc, s, 64);
+            if (lane >= s) inc += o;
         }
         __syncthreads();
-        for (int i = 0; i < n; ++i) {
-            const T* p = dy + (t0 + hit_t[i]) * cols + c0;
-            float* a = acc + hit_r[i] * ECOLS;
-            for (int c = tid; c < nc; c += NT) a[c] += to_f(p[c]);
+        if (lane == 63) wsum[wave] = inc;
+        __syncthreads();
+        uint32_t base = carry, all = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) {
+            if (w < wave) base += wsum[w];
+            all += wsum[w];
         }
+        base += inc - t;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            x[i0 + 4 * tid + k] = base;
+            base += v[k];
+        }
+        carry += all;
+    }
+    __syncthreads();
+}
+
+// Blocks `first` .. of a launch write zeros over dtable (n floats, a multiple of 8).
+template <int THREADS> __device__ __forceinline__ void fill(float* p, int64_t n, int first) {
+    const int64_t step = (int64_t)((int)gridDim.x - first) * THREADS * 4;
+    for (int64_t i = ((int64_t)((int)blockIdx.x - first) * THREADS + threadIdx.x) * 4; i < n; i += step)
+        *reinterpret_cast<floatx4*>(p + i) = floatx4{0.f, 0.f, 0.f, 0.f};
+}
+
+// Block 0 sorts, the others fill.  LDS: two arrays of `cap` packed (id,
+// token), the counters of each digit and wave, the waves' sums.
+__global__ __launch_bounds__(SORT_NT) void sort_fill_k(int tokens, int vocab, const int32_t* ids, int pad, int key_bits,
+                                                      int cap, uint32_t* keys, uint32_t* toks, float* dtable, int64_t n) {
+    extern __shared__ uint32_t sm[];
+    if (blockIdx.x > 0) {
+        fill<SORT_NT>(dtable, n, 1);
+        return;
+    }
+    uint32_t *a = sm, *b = sm + cap, *cnt = sm + 2 * cap, *wsum = cnt + BINS * SORT_W;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int per = (tokens + SORT_NT - 1) / SORT_NT * 64, i0 = wave * per, i1 = min(tokens, i0 + per);
+    for (int t = tid; t < tokens; t += SORT_NT) a[t] = key_of(ids[t], vocab, pad) << IDX_BITS | (uint32_t)t;
+    for (int shift = IDX_BITS; shift < IDX_BITS + key_bits; shift += 8) {
+        for (int i = tid; i < BINS * SORT_W; i += SORT_NT) cnt[i] = 0;
+        __syncthreads();
+        for (int i = i0; i < i1; i += 64) {
+            const bool in = i + lane < i1;
+            const uint32_t d = in ? a[i + lane] >> shift & (BINS - 1) : 0;
+            const uint64_t m = same_digit(d, in);
+            if (in && (m & ((1ull << lane) - 1)) == 0) cnt[d * SORT_W + wave] += (uint32_t)__popcll(m);
+        }
+        __syncthreads();
+        scan_lds<SORT_NT>(cnt, BINS * SORT_W, wsum);
+        for (int i = i0; i < i1; i += 64) {
+            const bool in = i + lane < i1;
+            const uint32_t x = in ? a[i + lane] : 0, d = x >> shift & (BINS - 1);
+            const uint64_t m = same_digit(d, in), below = m & ((1ull << lane) - 1);
+            uint32_t at = 0;
+            if (in) {
+                at = cnt[d * SORT_W + wave];
+                b[at + (uint32_t)__popcll(below)] = x;
+            }
+            // (the lanes of a wave run together: all have read the counter)
+            __builtin_amdgcn_wave_barrier();
+            if (in && below == 0) cnt[d * SORT_W + wave] = at + (uint32_t)__popcll(m);
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+        uint32_t* t = a;
+        a = b;
+        b = t;
+    }
+    for (int t = tid; t < tokens; t += SORT_NT) {
+        keys[t] = a[t] >> IDX_BITS;
+        toks[t] = a[t] & ((1u << IDX_BITS) - 1);
+    }
+}
+
+// One pass of the sort over blocks of `per` tokens (a multiple of PASS_NT).
+struct PassArgs {
+    int tokens, per, nblk, shift, vocab, pad;
+    const int32_t* ids;               // first pass: the ids; else null
+    const uint32_t *k_in, *t_in;
+    uint32_t *k_out, *t_out, *table;  // table [BINS][nblk]
+    float* dtable;                    // first pass: filled by the blocks behind nblk
+    int64_t n;
+};
+__device__ __forceinline__ uint32_t pass_key(const PassArgs& g, int i) {
+    return g.ids ? key_of(g.ids[i], g.vocab, g.pad) : g.k_in[i];
+}
+
+// cnt[wave][digit] of this block's tokens
+__device__ __forceinline__ void pass_count(const PassArgs& g, uint32_t* cnt, int i0, int i1) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    for (int i = tid; i < BINS * PASS_W; i += PASS_NT) cnt[i] = 0;
+    __syncthreads();
+    for (int i = i0; i < i1; i += 64) {
+        const bool in = i + lane < i1;
+        const uint32_t d = in ? pass_key(g, i + lane) >> g.shift & (BINS - 1) : 0;
+        const uint64_t m = same_digit(d, in);
+        if (in && (m & ((1ull << lane) - 1)) == 0) cnt[wave * BINS + d] += (uint32_t)__popcll(m);
+    }
+    __syncthreads();
+}
+
+__global__ __launch_bounds__(PASS_NT) void pass_count_k(PassArgs g) {
+    __shared__ uint32_t cnt[BINS * PASS_W];
+    if ((int)blockIdx.x >= g.nblk) {
+        fill<PASS_NT>(g.dtable, g.n, g.nblk);
+        return;
+    }
+    const int wave = threadIdx.x >> 6, end = min(g.tokens, ((int)blockIdx.x + 1) * g.per);
+    const int i0 = (int)blockIdx.x * g.per + wave * (g.per / PASS_W);
+    pass_count(g, cnt, i0, min(end, i0 + g.per / PASS_W));
+    uint32_t c = 0;
+#pragma unroll
+    for (int w = 0; w < PASS_W; ++w) c += cnt[w * BINS + threadIdx.x];
+    g.table[threadIdx.x * g.nblk + blockIdx.x] = c;
+}
+
+// Exclusive sums over the table, by one block.
+__global__ __launch_bounds__(SORT_NT) void pass_scan_k(uint32_t* table, int n) {
+    __shared__ uint32_t x[4 * SORT_NT], wsum[SORT_W];
+    uint32_t carry = 0;
+    for (int i0 = 0; i0 < n; i0 += 4 * SORT_NT) {
+        uint32_t last = 0;
+        for (int k = threadIdx.x; k < 4 * SORT_NT; k += SORT_NT) x[k] = i0 + k < n ? table[i0 + k] : 0;
+        __syncthreads();
+        last = x[4 * SORT_NT - 1];
+        __syncthreads();
+        scan_lds<SORT_NT>(x, 4 * SORT_NT, wsum);
+        for (int k = threadIdx.x; k < 4 * SORT_NT; k += SORT_NT)
+            if (i0 + k < n) table[i0 + k] = x[k] + carry;
+        carry += x[4 * SORT_NT - 1] + last;
         __syncthreads();
     }
-    for (int r = 0; r < EROWS && v0 + r < vocab; ++r)
-        for (int c = tid; c < nc; c += NT) dtable[(int64_t)(v0 + r) * cols + c0 + c] = acc[r * ECOLS + c] * scale;
+}
+
+__global__ __launch_bounds__(PASS_NT) void pass_place_k(PassArgs g) {
+    __shared__ uint32_t cnt[BINS * PASS_W];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int end = min(g.tokens, ((int)blockIdx.x + 1) * g.per);
+    const int i0 = (int)blockIdx.x * g.per + wave * (g.per / PASS_W), i1 = min(end, i0 + g.per / PASS_W);
+    pass_count(g, cnt, i0, i1);
+    uint32_t at = g.table[tid * g.nblk + blockIdx.x];
+#pragma unroll
+    for (int w = 0; w < PASS_W; ++w) {
+        const uint32_t c = cnt[w * BINS + tid];
+        cnt[w * BINS + tid] = at;
+        at += c;
+    }
+    __syncthreads();
+    for (int i = i0; i < i1; i += 64) {
+        const bool in = i + lane < i1;
+        const uint32_t k = in ? pass_key(g, i + lane) : 0, d = k >> g.shift & (BINS - 1);
+        const uint64_t m = same_digit(d, in), below = m & ((1ull << lane) - 1);
+        uint32_t base = 0;
+        if (in) {
+            base = cnt[wave * BINS + d];
+            const uint32_t to = base + (uint32_t)__popcll(below);
+            g.k_out[to] = k;
+            g.t_out[to] = g.ids ? (uint32_t)(i + lane) : g.t_in[i + lane];
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (in && below == 0) cnt[wave * BINS + d] = base + (uint32_t)__popcll(m);
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Where the sums of sorted tokens go.
+struct SumArgs {
+    int tokens, vocab, cols;
+    const uint32_t *keys, *toks;
+    const void* dy;
+    float scale;
+    float* dtable;
+    float* part;  // [pieces][2][cols]: first and last id's part; null: ids are followed to their end
+};
+
+// A wave takes 32 sorted tokens and 512 columns (8 a lane).
+template <typename T>
+__global__ __launch_bounds__(NT) void sum_k(SumArgs g) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int pieces = (g.tokens + PIECE - 1) / PIECE, slabs = (g.cols + 511) / 512;
+    const int64_t id = (int64_t)blockIdx.x * (NT / 64) + wave;
+    if (id >= (int64_t)pieces * slabs) return;
+    const int piece = (int)(id / slabs), col = (int)(id - (int64_t)piece * slabs) * 512 + lane * 8;
+    const bool in = col < g.cols;
+    int i = piece * PIECE, end = min(g.tokens, i + PIECE);
+    const uint32_t before = i > 0 ? g.keys[i - 1] : ~0u;
+    const uint32_t first = g.keys[i];
+    if (!g.part) {
+        // ids that began here, to their end
+        i += (int)__popcll(__ballot(i + lane < end && g.keys[min(i + lane, end - 1)] == before));
+        if (i == end) return;
+        const uint32_t k = g.keys[end - 1];
+        for (;;) {
+            const uint64_t m = __ballot(end + lane < g.tokens && g.keys[min(end + lane, g.tokens - 1)] == k);
+            end += (int)__popcll(m);
+            if (m != ~0ull) break;
+        }
+    }
+    const uint32_t after = end < g.tokens ? g.keys[end] : ~0u;
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const T* dy = reinterpret_cast<const T*>(g.dy) + col;
+    for (; i < end; i += PIECE) {
+        const int n = min(PIECE, end - i), me = i + min(lane, n - 1);
+        const uint32_t my_key = g.keys[me], my_tok = g.toks[me];
+        const uint32_t ahead = i + n < end ? g.keys[i + n] : after;
+        constexpr int U = 8;  // rows requested together
+        for (int s = 0; s < n; s += U) {
+            float x[U][8];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int at = min(s + u, n - 1);
+                const uint32_t k = __builtin_amdgcn_readlane(my_key, at), t = __builtin_amdgcn_readlane(my_tok, at);
+                if (in && k < (uint32_t)g.vocab) V8<T>::load(dy + (int64_t)t * g.cols, x[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (s + u >= n) break;
+                const uint32_t k = __builtin_amdgcn_readlane(my_key, s + u);
+                if (k >= (uint32_t)g.vocab) return;  // ids without a gradient are the last
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] += x[u][e];
+                const uint32_t nk = s + u + 1 < n ? __builtin_amdgcn_readlane(my_key, s + u + 1) : ahead;
+                const bool done = s + u + 1 == n && i + n == end;  // of this piece
+                if (nk == k && !done) continue;
+                // the id ends here, or the piece does
+                float* to = g.dtable + (int64_t)k * g.cols;
+                bool whole = true;
+                if (g.part) {
+                    if (k == first && before == first) {
+                        to = g.part + (int64_t)piece * 2 * g.cols;
+                        whole = false;
+                    } else if (nk == k) {
+                        to = g.part + ((int64_t)piece * 2 + 1) * g.cols;
+                        whole = false;
+                    }
+                }
+                if (in) {
+                    if (whole) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) acc[e] *= g.scale;
+                    }
+                    V8<float>::store(to + col, acc);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+            }
+        }
+    }
+}
+
+// Joins the parts of the ids that begin in a piece and end in a later one.
+__global__ __launch_bounds__(NT) void join_parts_k(SumArgs g) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int pieces = (g.tokens + PIECE - 1) / PIECE, slabs = (g.cols + 511) / 512;
+    const int64_t id = (int64_t)blockIdx.x * (NT / 64) + wave;
+    if (id >= (int64_t)pieces * slabs) return;
+    int piece = (int)(id / slabs);
+    const int col = (int)(id - (int64_t)piece * slabs) * 512 + lane * 8;
+    const int i = piece * PIECE, last = i + PIECE - 1;
+    if (last + 1 >= g.tokens) return;
+    const uint32_t k = g.keys[last];
+    if (k >= (uint32_t)g.vocab || g.keys[last + 1] != k) return;
+    if (i > 0 && g.keys[i] == k && g.keys[i - 1] == k) return;  // began earlier
+    if (col >= g.cols) return;
+    float acc[8];
+    V8<float>::load(g.part + ((int64_t)piece * 2 + 1) * g.cols + col, acc);
+    for (;;) {
+        ++piece;
+        float x[8];
+        V8<float>::load(g.part + (int64_t)piece * 2 * g.cols + col, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += x[e];
+        const int e = min(g.tokens, (piece + 1) * PIECE);
+        if (e >= g.tokens || g.keys[e - 1] != k || g.keys[e] != k) break;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] *= g.scale;
+    V8<float>::store(g.dtable + (int64_t)k * g.cols + col, acc);
+}
+
+constexpr size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+int key_bits(int vocab) { return 32 - __builtin_clz((unsigned)vocab); }  // of 0 .. vocab
+bool sorted_by_one(int64_t tokens, int vocab) { return tokens <= SORT_TOKENS && key_bits(vocab) <= 32 - IDX_BITS; }
+
+// Workspace: keys and tokens (two of each where the sort takes passes), the
+// passes' table, the parts.
+struct EmbedWs {
+    size_t list, table, part, bytes;
+    int per, nblk;
+};
+EmbedWs embed_ws(int64_t tokens, int vocab, int cols) {
+    EmbedWs w{};
+    w.list = align256((size_t)tokens * 4);
+    size_t at = 2 * w.list;
+    if (!sorted_by_one(tokens, vocab)) {
+        at = 4 * w.list;
+        w.per = 4096;
+        while ((tokens + w.per - 1) / w.per > PASS_BLOCKS) w.per *= 2;
+        w.nblk = (int)((tokens + w.per - 1) / w.per);
+        w.table = at;
+        at += align256((size_t)BINS * w.nblk * 4);
+    }
+    w.part = at;
+    if (tokens > RUN_TOKENS) at += align256((size_t)((tokens + PIECE - 1) / PIECE) * 2 * cols * 4);
+    w.bytes = at;
+    return w;
+}
+
+template <typename T>
+void launch_sums(const SumArgs& a, hipStream_t st) {
+    const int64_t waves = (int64_t)((a.tokens + PIECE - 1) / PIECE) * ((a.cols + 511) / 512);
+    const dim3 grid((unsigned)((waves + NT / 64 - 1) / (NT / 64)));
+    sum_k<T><<<grid, NT, 0, st>>>(a);
+    if (a.part) join_parts_k<<<grid, NT, 0, st>>>(a);
 }
 
 int check_embed(int32_t dtype, int64_t tokens, int32_t vocab, int32_t cols, float scale) {
     DM_TRY(check_dtype(dtype));
     DM_TRY(check_rows(tokens, cols, 16384));
-    if (tokens > INT32_MAX) return set_error(DM_ERR_UNSUPPORTED, "more than 2^31 - 1 tokens");
+    if (tokens > (1 << 30)) return set_error(DM_ERR_UNSUPPORTED, "more than 2^30 tokens");
     if (vocab <= 0) return set_error(DM_ERR_ARG, "vocab=%d", vocab);
     if (!(scale - scale == 0.f)) return set_error(DM_ERR_ARG, "scale=%g", scale);
     return DM_OK;
@@ -88,13 +420,6 @@ void launch_fwd(int64_t tokens, int vocab, int cols, const int32_t* ids, const v
     embed_fwd_k<T><<<dim3((unsigned)((tokens + tpb - 1) / tpb)), NT, 0, st>>>(tokens, vocab, cols, lanes, ids,
                                                                              (const T*)table, scale, (T*)y);
 }
-template <typename T>
-void launch_bwd(int64_t tokens, int vocab, int cols, const int32_t* ids, int pad, const void* dy, float scale,
-                float* dtable, hipStream_t st) {
-    const dim3 grid((unsigned)(((int64_t)vocab + EROWS - 1) / EROWS), (unsigned)((cols + ECOLS - 1) / ECOLS));
-    embed_bwd_k<T><<<grid, NT, 0, st>>>(tokens, vocab, cols, ids, pad, (const T*)dy, scale, dtable);
-}
-
 }  // namespace
 }  // namespace dm
 
@@ -103,8 +428,8 @@ using namespace dm;
 extern "C" {
 
 size_t embed_ws_bytes(int64_t tokens, int32_t vocab, int32_t cols) {
-    (void)tokens; (void)vocab; (void)cols;
-    return 0;
+    if (tokens <= 0 || tokens > (1 << 30) || vocab <= 0 || cols <= 0) return 0;
+    return embed_ws(tokens, vocab, cols).bytes;
 }
 
 int embed_fwd(int32_t dtype, int64_t tokens, int32_t vocab, int32_t cols, const int32_t* ids, const void* table,
@@ -131,9 +456,48 @@ int embed_bwd(int32_t dtype, int64_t tokens, int32_t vocab, int32_t cols, const 
     if (ws_bytes < need) return set_error(DM_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws_bytes, need);
     if (need) DM_TRY(check_ptr(ws, "ws"));
     const hipStream_t st = S(stream);
-    if (dtype == DM_F16) launch_bwd<half_t>(tokens, vocab, cols, ids, pad_id, dy, scale, dtable, st);
-    else if (dtype == DM_BF16) launch_bwd<bf16_t>(tokens, vocab, cols, ids, pad_id, dy, scale, dtable, st);
-    else launch_bwd<float>(tokens, vocab, cols, ids, pad_id, dy, scale, dtable, st);
+    const int64_t n = (int64_t)vocab * cols;
+    // zeros: blocks of 64 KB, up to four for each of the 256 CUs
+    const int64_t fills = std::min<int64_t>((n + 16383) / 16384, 1024);
+    const EmbedWs w = tokens > 0 ? embed_ws(tokens, vocab, cols) : EmbedWs{};
+    uint32_t* keys = (uint32_t*)ws;
+    uint32_t* toks = (uint32_t*)((char*)ws + w.list);
+    if (tokens == 0 || sorted_by_one(tokens, vocab)) {
+        const int cap = ((int)tokens + 63) / 64 * 64;
+        const size_t lds = (size_t)(2 * cap + BINS * SORT_W + SORT_W) * 4;
+        if (lds > 65536)
+            (void)hipFuncSetAttribute(reinterpret_cast<const void*>(sort_fill_k),
+                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        sort_fill_k<<<dim3((unsigned)(1 + fills)), SORT_NT, lds, st>>>((int)tokens, vocab, ids, pad_id, key_bits(vocab), cap,
+                                                                      keys, toks, dtable, n);
+    } else {
+        PassArgs a{};
+        a.tokens = (int)tokens; a.per = w.per; a.nblk = w.nblk; a.vocab = vocab; a.pad = pad_id;
+        a.ids = ids; a.table = (uint32_t*)((char*)ws + w.table);
+        a.dtable = dtable; a.n = n;
+        uint32_t* list[2][2] = {{keys, toks}, {(uint32_t*)((char*)ws + 2 * w.list), (uint32_t*)((char*)ws + 3 * w.list)}};
+        int to = 0;
+        for (a.shift = 0; a.shift < key_bits(vocab); a.shift += 8) {
+            a.k_out = list[to][0];
+            a.t_out = list[to][1];
+            pass_count_k<<<dim3((unsigned)(w.nblk + (a.ids ? fills : 0))), PASS_NT, 0, st>>>(a);
+            pass_scan_k<<<dim3(1), SORT_NT, 0, st>>>(a.table, BINS * w.nblk);
+            pass_place_k<<<dim3((unsigned)w.nblk), PASS_NT, 0, st>>>(a);
+            a.ids = nullptr;
+            a.k_in = keys = list[to][0];
+            a.t_in = toks = list[to][1];
+            to ^= 1;
+        }
+    }
+    if (tokens > 0) {
+        SumArgs a{};
+        a.tokens = (int)tokens; a.vocab = vocab; a.cols = cols;
+        a.keys = keys; a.toks = toks; a.dy = dy; a.scale = scale; a.dtable = dtable;
+        if (tokens > RUN_TOKENS) a.part = (float*)((char*)ws + w.part);
+        if (dtype == DM_F16) launch_sums<half_t>(a, st);
+        else if (dtype == DM_BF16) launch_sums<bf16_t>(a, st);
+        else launch_sums<float>(a, st);
+    }
     return check_launch("embed_bwd");
 }
 
