@@ -32,21 +32,28 @@ __global__ __launch_bounds__(NT) void embed_fwd_k(int64_t tokens, int vocab, int
 // ------------------------------------------------------------ gradient
 // dtable[v] = scale sum over the tokens of id v: the tokens are sorted by id
 // (stable: the order of the sums is given by the ids alone), then every
-// wave adds up 32 neighbours of the sorted list, writing the rows whose
-// tokens all lie there and leaving partial sums of the first and the last
-// otherwise, which a last pass joins in order.  So the work is even however
-// often an id occurs, dy is read once, and rows that no token has come from
-// the fill that runs beside the sort: the pass is bound by writing dtable
-// and reading dy.
+// wave adds up a piece of the sorted list, writing the rows whose tokens all
+// lie there and leaving partial sums of the first and the last otherwise,
+// which a last pass joins in order.  So the work is even however often an id
+// occurs, dy is read once, and rows that no token has come from the fill
+// that runs beside the sort: the pass is bound by writing dtable and reading
+// dy.
 //
-// Up to 16384 tokens are sorted by one block in LDS while the other blocks
-// fill; more by passes over blocks of tokens (count, scan, place).
-constexpr int PIECE = 32;          // sorted tokens of a wave
+// The sort: up to 16384 tokens in lists of 1024, each by one block in LDS
+// while the other blocks of the launch fill; a second launch places every
+// token by counting, in each list, what comes before it.  (One block for all
+// 16384 takes 52 us: the ballots of a radix pass are bound by its CU's
+// vector units.)  More tokens by passes over blocks of tokens (count, scan,
+// place).
+constexpr int PIECE = 8;           // sorted tokens of a wave, all requested together
+constexpr int PIECE_FEW = 4;       // up to RUN_TOKENS tokens: shorter chains
 constexpr int RUN_TOKENS = 1024;   // up to here a wave follows its last id to the end instead of leaving it in parts:
                                    // one launch less where launches are what counts
 constexpr int SORT_TOKENS = 16384;
-constexpr int IDX_BITS = 14;       // of a token's number in the one-block sort, below its id
+constexpr int IDX_BITS = 14;       // of a token's number in the sort of lists, below its id
+constexpr int LIST = 1024;         // tokens of a list
 constexpr int SORT_NT = 1024, SORT_W = SORT_NT / 64;
+constexpr int LIST_NT = 256, LIST_W = LIST_NT / 64;
 constexpr int BINS = 256;          // of a pass: 8 bits
 constexpr int PASS_NT = 256, PASS_W = PASS_NT / 64;
 constexpr int PASS_BLOCKS = 1024;
@@ -111,42 +118,45 @@ template <int THREADS> __device__ __forceinline__ void fill(float* p, int64_t n,
         *reinterpret_cast<floatx4*>(p + i) = floatx4{0.f, 0.f, 0.f, 0.f};
 }
 
-// Block 0 sorts, the others fill.  LDS: two arrays of `cap` packed (id,
-// token), the counters of each digit and wave, the waves' sums.
-__global__ __launch_bounds__(SORT_NT) void sort_fill_k(int tokens, int vocab, const int32_t* ids, int pad, int key_bits,
-                                                      int cap, uint32_t* keys, uint32_t* toks, float* dtable, int64_t n) {
-    extern __shared__ uint32_t sm[];
-    if (blockIdx.x > 0) {
-        fill<SORT_NT>(dtable, n, 1);
+// Blocks 0 .. lists - 1 sort 1024 tokens each, the others fill.  A list
+// holds (id, token) packed, so that all differ and their order is the
+// stable one.  With one list, the result is the final one.
+__global__ __launch_bounds__(LIST_NT) void sort_fill_k(int tokens, int lists, int vocab, const int32_t* ids, int pad,
+                                                      int key_bits, uint32_t* packed, uint32_t* keys, uint32_t* toks,
+                                                      float* dtable, int64_t n) {
+    __shared__ uint32_t mem[2][LIST], cnt[BINS * LIST_W], wsum[LIST_W];
+    if ((int)blockIdx.x >= lists) {
+        fill<LIST_NT>(dtable, n, lists);
         return;
     }
-    uint32_t *a = sm, *b = sm + cap, *cnt = sm + 2 * cap, *wsum = cnt + BINS * SORT_W;
+    uint32_t *a = mem[0], *b = mem[1];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int per = (tokens + SORT_NT - 1) / SORT_NT * 64, i0 = wave * per, i1 = min(tokens, i0 + per);
-    for (int t = tid; t < tokens; t += SORT_NT) a[t] = key_of(ids[t], vocab, pad) << IDX_BITS | (uint32_t)t;
+    const int t0 = (int)blockIdx.x * LIST, len = min(LIST, tokens - t0);
+    const int i0 = wave * (LIST / LIST_W), i1 = min(len, i0 + LIST / LIST_W);
+    for (int t = tid; t < len; t += LIST_NT) a[t] = key_of(ids[t0 + t], vocab, pad) << IDX_BITS | (uint32_t)(t0 + t);
     for (int shift = IDX_BITS; shift < IDX_BITS + key_bits; shift += 8) {
-        for (int i = tid; i < BINS * SORT_W; i += SORT_NT) cnt[i] = 0;
+        for (int i = tid; i < BINS * LIST_W; i += LIST_NT) cnt[i] = 0;
         __syncthreads();
         for (int i = i0; i < i1; i += 64) {
             const bool in = i + lane < i1;
             const uint32_t d = in ? a[i + lane] >> shift & (BINS - 1) : 0;
             const uint64_t m = same_digit(d, in);
-            if (in && (m & ((1ull << lane) - 1)) == 0) cnt[d * SORT_W + wave] += (uint32_t)__popcll(m);
+            if (in && (m & ((1ull << lane) - 1)) == 0) cnt[d * LIST_W + wave] += (uint32_t)__popcll(m);
         }
         __syncthreads();
-        scan_lds<SORT_NT>(cnt, BINS * SORT_W, wsum);
+        scan_lds<LIST_NT>(cnt, BINS * LIST_W, wsum);
         for (int i = i0; i < i1; i += 64) {
             const bool in = i + lane < i1;
             const uint32_t x = in ? a[i + lane] : 0, d = x >> shift & (BINS - 1);
             const uint64_t m = same_digit(d, in), below = m & ((1ull << lane) - 1);
             uint32_t at = 0;
             if (in) {
-                at = cnt[d * SORT_W + wave];
+                at = cnt[d * LIST_W + wave];
                 b[at + (uint32_t)__popcll(below)] = x;
             }
             // (the lanes of a wave run together: all have read the counter)
             __builtin_amdgcn_wave_barrier();
-            if (in && below == 0) cnt[d * SORT_W + wave] = at + (uint32_t)__popcll(m);
+            if (in && below == 0) cnt[d * LIST_W + wave] = at + (uint32_t)__popcll(m);
             __builtin_amdgcn_wave_barrier();
         }
         __syncthreads();
@@ -154,10 +164,48 @@ __global__ __launch_bounds__(SORT_NT) void sort_fill_k(int tokens, int vocab, co
         a = b;
         b = t;
     }
-    for (int t = tid; t < tokens; t += SORT_NT) {
-        keys[t] = a[t] >> IDX_BITS;
-        toks[t] = a[t] & ((1u << IDX_BITS) - 1);
+    for (int t = tid; t < len; t += LIST_NT) {
+        if (lists == 1) {
+            keys[t] = a[t] >> IDX_BITS;
+            toks[t] = a[t] & ((1u << IDX_BITS) - 1);
+        } else {
+            packed[t0 + t] = a[t];
+        }
     }
+}
+
+// Every token's place: what comes before it in its own list and in the others.
+__global__ __launch_bounds__(LIST_NT) void merge_k(int tokens, const uint32_t* packed, uint32_t* keys, uint32_t* toks) {
+    __shared__ __attribute__((aligned(16))) uint32_t x[SORT_TOKENS];
+    __shared__ int place[LIST_W][64];
+    u32x4 r[SORT_TOKENS / (LIST_NT * 4)];  // all requested together (packed has room to a multiple of 64)
+#pragma unroll
+    for (int k = 0; k < SORT_TOKENS / (LIST_NT * 4); ++k)
+        r[k] = *reinterpret_cast<const u32x4*>(packed + min((k * LIST_NT + (int)threadIdx.x) * 4, (tokens - 1) & ~3));
+#pragma unroll
+    for (int k = 0; k < SORT_TOKENS / (LIST_NT * 4); ++k)
+        *reinterpret_cast<u32x4*>(x + (k * LIST_NT + threadIdx.x) * 4) = r[k];
+    __syncthreads();
+    // 64 tokens a block; each wave searches a quarter of the lists for them,
+    // side by side, so that their steps wait together
+    constexpr int U = SORT_TOKENS / LIST / LIST_W;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = (int)blockIdx.x * 64 + lane;
+    const uint32_t p = x[min(i, tokens - 1)];
+    // how many of each list's are below p (in its own list: the token's place there)
+    int lo[U] = {0, 0, 0, 0};
+#pragma unroll
+    for (int step = LIST; step > 0; step >>= 1)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int h = lo[u] + step, q = (wave * U + u) * LIST + h - 1;
+            if (h <= LIST && q < tokens && x[min(q, SORT_TOKENS - 1)] < p) lo[u] = h;
+        }
+    place[wave][lane] = lo[0] + lo[1] + lo[2] + lo[3];
+    __syncthreads();
+    if (wave > 0 || i >= tokens) return;
+    const int at = place[0][lane] + place[1][lane] + place[2][lane] + place[3][lane];
+    keys[at] = p >> IDX_BITS;
+    toks[at] = p & ((1u << IDX_BITS) - 1);
 }
 
 // One pass of the sort over blocks of `per` tokens (a multiple of PASS_NT).
@@ -261,23 +309,48 @@ struct SumArgs {
     float* part;  // [pieces][2][cols]: first and last id's part; null: ids are followed to their end
 };
 
-// A wave takes 32 sorted tokens and 512 columns (8 a lane).
-template <typename T>
+// 8 elements as they lie in memory
+template <typename T> struct Raw8 {
+    u32x4 v[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(T) / 2); ++i) v[i] = reinterpret_cast<const u32x4*>(p)[i];
+    }
+    __device__ __forceinline__ void add_to(float acc[8]) const {
+        float x[8];
+        if constexpr (sizeof(T) == 2) {
+            V8<T>::unpack(v[0], x);
+        } else {
+            const floatx4 a = __builtin_bit_cast(floatx4, v[0]), b = __builtin_bit_cast(floatx4, v[1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] += x[i];
+    }
+};
+
+// A wave takes PC sorted tokens and 512 columns (8 a lane; lanes past the
+// last column read the last ones again and store nothing).
+template <typename T, int PC>
 __global__ __launch_bounds__(NT) void sum_k(SumArgs g) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int pieces = (g.tokens + PIECE - 1) / PIECE, slabs = (g.cols + 511) / 512;
+    const int pieces = (g.tokens + PC - 1) / PC, slabs = (g.cols + 511) / 512;
     const int64_t id = (int64_t)blockIdx.x * (NT / 64) + wave;
     if (id >= (int64_t)pieces * slabs) return;
     const int piece = (int)(id / slabs), col = (int)(id - (int64_t)piece * slabs) * 512 + lane * 8;
     const bool in = col < g.cols;
-    int i = piece * PIECE, end = min(g.tokens, i + PIECE);
+    int i = piece * PC, end = min(g.tokens, i + PC);
+    // the piece's keys and its neighbours', requested together
+    const uint32_t key0 = g.keys[min(i + lane, g.tokens - 1)];
     const uint32_t before = i > 0 ? g.keys[i - 1] : ~0u;
-    const uint32_t first = g.keys[i];
+    const uint32_t first = __builtin_amdgcn_readlane(key0, 0);
+    if (first >= (uint32_t)g.vocab) return;  // ids without a gradient are the last
     if (!g.part) {
         // ids that began here, to their end
-        i += (int)__popcll(__ballot(i + lane < end && g.keys[min(i + lane, end - 1)] == before));
+        const uint32_t k = __builtin_amdgcn_readlane(key0, end - 1 - i);
+        i += (int)__popcll(__ballot(i + lane < end && key0 == before));
         if (i == end) return;
-        const uint32_t k = g.keys[end - 1];
         for (;;) {
             const uint64_t m = __ballot(end + lane < g.tokens && g.keys[min(end + lane, g.tokens - 1)] == k);
             end += (int)__popcll(m);
@@ -286,92 +359,91 @@ __global__ __launch_bounds__(NT) void sum_k(SumArgs g) {
     }
     const uint32_t after = end < g.tokens ? g.keys[end] : ~0u;
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const T* dy = reinterpret_cast<const T*>(g.dy) + col;
-    for (; i < end; i += PIECE) {
-        const int n = min(PIECE, end - i), me = i + min(lane, n - 1);
+    const T* dy = reinterpret_cast<const T*>(g.dy) + min(col, g.cols - 8);
+    for (; i < end; i += PC) {
+        const int n = min(PC, end - i), me = i + min(lane, n - 1);
         const uint32_t my_key = g.keys[me], my_tok = g.toks[me];
         const uint32_t ahead = i + n < end ? g.keys[i + n] : after;
-        constexpr int U = 8;  // rows requested together
-        for (int s = 0; s < n; s += U) {
-            float x[U][8];
+        Raw8<T> x[PC];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int at = min(s + u, n - 1);
-                const uint32_t k = __builtin_amdgcn_readlane(my_key, at), t = __builtin_amdgcn_readlane(my_tok, at);
-                if (in && k < (uint32_t)g.vocab) V8<T>::load(dy + (int64_t)t * g.cols, x[u]);
+        for (int u = 0; u < PC; ++u)
+            x[u].load(dy + (int64_t)__builtin_amdgcn_readlane(my_tok, min(u, n - 1)) * g.cols);
+#pragma unroll
+        for (int u = 0; u < PC; ++u) {
+            if (u >= n) break;
+            const uint32_t k = __builtin_amdgcn_readlane(my_key, u);
+            if (k >= (uint32_t)g.vocab) return;
+            x[u].add_to(acc);
+            const uint32_t nk = u + 1 < n ? __builtin_amdgcn_readlane(my_key, u + 1) : ahead;
+            const bool done = u + 1 == n && i + n == end;  // of this piece
+            if (nk == k && !done) continue;
+            // the id ends here, or the piece does
+            float* to = g.dtable + (int64_t)k * g.cols;
+            bool whole = true;
+            if (g.part) {
+                if (k == first && before == first) {
+                    to = g.part + (int64_t)piece * 2 * g.cols;
+                    whole = false;
+                } else if (nk == k) {
+                    to = g.part + ((int64_t)piece * 2 + 1) * g.cols;
+                    whole = false;
+                }
+            }
+            if (in) {
+                if (whole) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) acc[e] *= g.scale;
+                }
+                V8<float>::store(to + col, acc);
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (s + u >= n) break;
-                const uint32_t k = __builtin_amdgcn_readlane(my_key, s + u);
-                if (k >= (uint32_t)g.vocab) return;  // ids without a gradient are the last
-#pragma unroll
-                for (int e = 0; e < 8; ++e) acc[e] += x[u][e];
-                const uint32_t nk = s + u + 1 < n ? __builtin_amdgcn_readlane(my_key, s + u + 1) : ahead;
-                const bool done = s + u + 1 == n && i + n == end;  // of this piece
-                if (nk == k && !done) continue;
-                // the id ends here, or the piece does
-                float* to = g.dtable + (int64_t)k * g.cols;
-                bool whole = true;
-                if (g.part) {
-                    if (k == first && before == first) {
-                        to = g.part + (int64_t)piece * 2 * g.cols;
-                        whole = false;
-                    } else if (nk == k) {
-                        to = g.part + ((int64_t)piece * 2 + 1) * g.cols;
-                        whole = false;
-                    }
-                }
-                if (in) {
-                    if (whole) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) acc[e] *= g.scale;
-                    }
-                    V8<float>::store(to + col, acc);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-            }
+            for (int e = 0; e < 8; ++e) acc[e] = 0.f;
         }
     }
 }
 
-// Joins the parts of the ids that begin in a piece and end in a later one.
+// Joins the parts of the ids that begin in a piece and end in a later one:
+// a wave takes 256 columns.
 __global__ __launch_bounds__(NT) void join_parts_k(SumArgs g) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int pieces = (g.tokens + PIECE - 1) / PIECE, slabs = (g.cols + 511) / 512;
+    const int pieces = (g.tokens + PIECE - 1) / PIECE, slabs = (g.cols + 255) / 256;
     const int64_t id = (int64_t)blockIdx.x * (NT / 64) + wave;
     if (id >= (int64_t)pieces * slabs) return;
-    int piece = (int)(id / slabs);
-    const int col = (int)(id - (int64_t)piece * slabs) * 512 + lane * 8;
+    const int piece = (int)(id / slabs);
+    const int col = (int)(id - (int64_t)piece * slabs) * 256 + lane * 4;
     const int i = piece * PIECE, last = i + PIECE - 1;
     if (last + 1 >= g.tokens) return;
-    const uint32_t k = g.keys[last];
-    if (k >= (uint32_t)g.vocab || g.keys[last + 1] != k) return;
-    if (i > 0 && g.keys[i] == k && g.keys[i - 1] == k) return;  // began earlier
-    if (col >= g.cols) return;
-    float acc[8];
-    V8<float>::load(g.part + ((int64_t)piece * 2 + 1) * g.cols + col, acc);
-    for (;;) {
-        ++piece;
-        float x[8];
-        V8<float>::load(g.part + (int64_t)piece * 2 * g.cols + col, x);
+    const uint32_t k = g.keys[last], next = g.keys[last + 1], first = g.keys[i], before = i > 0 ? g.keys[i - 1] : ~0u;
+    if (k >= (uint32_t)g.vocab || next != k) return;
+    if (first == k && before == k) return;  // began earlier
+    const float* part = g.part + min(col, g.cols - 4);
+    floatx4 acc = *reinterpret_cast<const floatx4*>(part + ((int64_t)piece * 2 + 1) * g.cols);
+    for (int p0 = piece + 1;; p0 += 64) {
+        // pieces that begin with the id: a run of the next ones
+        const int64_t at = ((int64_t)p0 + lane) * PIECE;
+        const uint64_t m = __ballot(at < g.tokens && g.keys[min(at, (int64_t)g.tokens - 1)] == k);
+        const int n = (int)__popcll(m);
+        constexpr int U = 32;  // requested together
+        for (int s = 0; s < n; s += U) {
+            floatx4 x[U];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += x[e];
-        const int e = min(g.tokens, (piece + 1) * PIECE);
-        if (e >= g.tokens || g.keys[e - 1] != k || g.keys[e] != k) break;
+            for (int u = 0; u < U; ++u)
+                x[u] = *reinterpret_cast<const floatx4*>(part + (int64_t)(p0 + min(s + u, n - 1)) * 2 * g.cols);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (s + u < n) acc += x[u];
+        }
+        if (n < 64) break;
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] *= g.scale;
-    V8<float>::store(g.dtable + (int64_t)k * g.cols + col, acc);
+    if (col < g.cols) *reinterpret_cast<floatx4*>(g.dtable + (int64_t)k * g.cols + col) = acc * g.scale;
 }
 
 constexpr size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 int key_bits(int vocab) { return 32 - __builtin_clz((unsigned)vocab); }  // of 0 .. vocab
-bool sorted_by_one(int64_t tokens, int vocab) { return tokens <= SORT_TOKENS && key_bits(vocab) <= 32 - IDX_BITS; }
+bool sorted_in_lists(int64_t tokens, int vocab) { return tokens <= SORT_TOKENS && key_bits(vocab) <= 32 - IDX_BITS; }
 
-// Workspace: keys and tokens (two of each where the sort takes passes), the
-// passes' table, the parts.
+// Workspace: keys and tokens, the lists (or, for passes, a second pair of
+// them and the table), the parts.
 struct EmbedWs {
     size_t list, table, part, bytes;
     int per, nblk;
@@ -379,8 +451,8 @@ struct EmbedWs {
 EmbedWs embed_ws(int64_t tokens, int vocab, int cols) {
     EmbedWs w{};
     w.list = align256((size_t)tokens * 4);
-    size_t at = 2 * w.list;
-    if (!sorted_by_one(tokens, vocab)) {
+    size_t at = 3 * w.list;
+    if (!sorted_in_lists(tokens, vocab)) {
         at = 4 * w.list;
         w.per = 4096;
         while ((tokens + w.per - 1) / w.per > PASS_BLOCKS) w.per *= 2;
@@ -396,10 +468,16 @@ EmbedWs embed_ws(int64_t tokens, int vocab, int cols) {
 
 template <typename T>
 void launch_sums(const SumArgs& a, hipStream_t st) {
-    const int64_t waves = (int64_t)((a.tokens + PIECE - 1) / PIECE) * ((a.cols + 511) / 512);
+    const int64_t pc = a.part ? PIECE : PIECE_FEW;
+    const int64_t waves = (a.tokens + pc - 1) / pc * ((a.cols + 511) / 512);
     const dim3 grid((unsigned)((waves + NT / 64 - 1) / (NT / 64)));
-    sum_k<T><<<grid, NT, 0, st>>>(a);
-    if (a.part) join_parts_k<<<grid, NT, 0, st>>>(a);
+    if (a.part) {
+        sum_k<T, PIECE><<<grid, NT, 0, st>>>(a);
+        const int64_t joins = (a.tokens + pc - 1) / pc * ((a.cols + 255) / 256);
+        join_parts_k<<<dim3((unsigned)((joins + NT / 64 - 1) / (NT / 64))), NT, 0, st>>>(a);
+    } else {
+        sum_k<T, PIECE_FEW><<<grid, NT, 0, st>>>(a);
+    }
 }
 
 int check_embed(int32_t dtype, int64_t tokens, int32_t vocab, int32_t cols, float scale) {
@@ -462,14 +540,13 @@ int embed_bwd(int32_t dtype, int64_t tokens, int32_t vocab, int32_t cols, const 
     const EmbedWs w = tokens > 0 ? embed_ws(tokens, vocab, cols) : EmbedWs{};
     uint32_t* keys = (uint32_t*)ws;
     uint32_t* toks = (uint32_t*)((char*)ws + w.list);
-    if (tokens == 0 || sorted_by_one(tokens, vocab)) {
-        const int cap = ((int)tokens + 63) / 64 * 64;
-        const size_t lds = (size_t)(2 * cap + BINS * SORT_W + SORT_W) * 4;
-        if (lds > 65536)
-            (void)hipFuncSetAttribute(reinterpret_cast<const void*>(sort_fill_k),
-                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        sort_fill_k<<<dim3((unsigned)(1 + fills)), SORT_NT, lds, st>>>((int)tokens, vocab, ids, pad_id, key_bits(vocab), cap,
-                                                                      keys, toks, dtable, n);
+    if (tokens == 0 || sorted_in_lists(tokens, vocab)) {
+        const int lists = (int)((tokens + LIST - 1) / LIST);
+        uint32_t* packed = (uint32_t*)((char*)ws + 2 * w.list);
+        sort_fill_k<<<dim3((unsigned)(lists + fills)), LIST_NT, 0, st>>>((int)tokens, lists, vocab, ids, pad_id,
+                                                                        key_bits(vocab), packed, keys, toks, dtable, n);
+        if (lists > 1)
+            merge_k<<<dim3((unsigned)((tokens + 63) / 64)), LIST_NT, 0, st>>>((int)tokens, packed, keys, toks);
     } else {
         PassArgs a{};
         a.tokens = (int)tokens; a.per = w.per; a.nblk = w.nblk; a.vocab = vocab; a.pad = pad_id;
