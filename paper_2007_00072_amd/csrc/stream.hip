@@ -33,11 +33,22 @@ int key_splits(const dm_attn_desc& d) {
     return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
 }
 
+// Parts the query heads of a key/value head are split into in the dK / dV
+// kernel, whose blocks otherwise walk all of them: four blocks for each CU
+// (causal ones differ in length), against the parts' sums in memory.
+int head_parts(const dm_attn_desc& d) {
+    const int grp = d.H / d.G;
+    const int64_t blocks = ((int64_t)d.K + STREAM_KEYS - 1) / STREAM_KEYS * d.B * d.G;
+    if (blocks == 0 || grp == 1) return 1;
+    const int64_t want = (1024 + blocks - 1) / blocks;
+    return (int)(want < grp ? want : grp);
+}
+
 struct Sizes {
     size_t lo, saved;                     // saved: lse, then lo
     size_t ranges, part_o, part_ml, fwd;  // forward workspace: ends of its parts
     size_t dsum, dmax, bwd;               // backward workspace (ranges first)
-    int splits, dmax_n;
+    int splits, dmax_n, hparts;
 };
 
 Sizes sizes_of(const dm_attn_desc& d) {
@@ -45,7 +56,7 @@ Sizes sizes_of(const dm_attn_desc& d) {
     const size_t rows = (size_t)d.B * d.H * d.J;
     s.lo = align256(rows * 4);
     s.saved = s.lo + (d.dtype == DM_F32 ? 0 : align256(rows * d.P * esize(d.dtype)));
-    s.ranges = d.doc ? align256((size_t)d.B * ((d.K + STREAM_RANGE - 1) / STREAM_RANGE) * sizeof(int2)) : 0;
+    s.ranges = d.doc ? align256((size_t)d.B * ((d.K + STREAM_RANGE - 1) / STREAM_RANGE) * sizeof(int4)) : 0;
     s.splits = key_splits(d);
     const size_t parts = s.splits > 1 ? (size_t)s.splits * rows : 0;
     s.part_o = s.ranges + align256(parts * d.P * 4);
@@ -54,14 +65,18 @@ Sizes sizes_of(const dm_attn_desc& d) {
     s.dmax_n = (d.J + STREAM_DROWS - 1) / STREAM_DROWS;
     s.dsum = s.ranges + align256(rows * 4);
     s.dmax = s.dsum + (d.dtype == DM_F16 ? align256((size_t)d.B * d.H * s.dmax_n * 4) : 0);
-    s.bwd = s.dmax;
+    s.hparts = head_parts(d);
+    s.bwd = s.dmax + (s.hparts > 1 ? align256((size_t)s.hparts * d.B * d.G * d.K * 2 * d.P * 4) : 0);
     return s;
 }
 
-int check_stride(const dm_attn_stride& s, const char* n) {
+int check_stride(const dm_attn_stride& s, int tokens, int P, const char* n) {
     if (s.b < 0 || s.h < 0 || s.t < 0) return set_error(DM_ERR_UNSUPPORTED, "%s: negative stride", n);
     if (s.b % 8 || s.h % 8 || s.t % 8)
         return set_error(DM_ERR_UNSUPPORTED, "%s: strides must be multiples of 8 elements", n);
+    // (a step's rows are addressed by 32-bit offsets from its first)
+    if (tokens > 1 && (s.t < P || s.t > (1 << 22)))
+        return set_error(DM_ERR_UNSUPPORTED, "%s: token stride %lld outside [P, 2^22]", n, (long long)s.t);
     return DM_OK;
 }
 
@@ -102,10 +117,10 @@ int check_desc(const dm_attn_desc* d) {
         return set_error(DM_ERR_ARG, "scaler=%g cap=%g", d->scaler, d->cap);
     if (d->causal != 0 && d->causal != 1) return set_error(DM_ERR_ARG, "causal=%d", d->causal);
     if (d->prefix && !d->causal) return set_error(DM_ERR_ARG, "prefix without causal: every key is seen already");
-    DM_TRY(check_stride(d->q, "q"));
-    DM_TRY(check_stride(d->k, "k"));
-    DM_TRY(check_stride(d->v, "v"));
-    DM_TRY(check_stride(d->out, "out"));
+    DM_TRY(check_stride(d->q, d->J, d->P, "q"));
+    DM_TRY(check_stride(d->k, d->K, d->P, "k"));
+    DM_TRY(check_stride(d->v, d->K, d->P, "v"));
+    DM_TRY(check_stride(d->out, d->J, d->P, "out"));
     return check_written(d->out, d->B, d->H, d->J, d->P, "out");
 }
 
@@ -159,7 +174,7 @@ int attn_fwd(const dm_attn_desc* d, const void* q, const void* k, const void* v,
         a.lse = (float*)saved;
         if (d->dtype != DM_F32) a.lo = (char*)saved + s.lo;
     }
-    a.ranges = (int2*)ws;
+    a.ranges = (int4*)ws;
     a.splits = s.splits;
     a.part_o = (float*)((char*)ws + s.ranges);
     a.part_ml = (float2*)((char*)ws + s.part_o);
@@ -194,10 +209,12 @@ int attn_bwd(const dm_attn_desc* d, const void* q, const void* k, const void* v,
     a.dout = rows_of(dout, d->out); a.dq = rows_of(dq, d->q); a.dk = rows_of(dk, d->k); a.dv = rows_of(dv, d->v);
     a.lse = (float*)saved;
     if (d->dtype != DM_F32) a.lo = (char*)saved + s.lo;
-    a.ranges = (int2*)ws;
+    a.ranges = (int4*)ws;
     a.dsum = (float*)((char*)ws + s.ranges);
     a.dmax = d->dtype == DM_F16 ? (float*)((char*)ws + s.dsum) : nullptr;
     a.dmax_n = s.dmax_n;
+    a.hparts = s.hparts;
+    a.part_k = (float*)((char*)ws + s.dmax);
     const hipStream_t st = S(stream);
     if (d->dtype == DM_F16) stream_bwd<half_t>(a, st);
     else if (d->dtype == DM_BF16) stream_bwd<bf16_t>(a, st);

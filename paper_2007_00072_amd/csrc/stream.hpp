@@ -23,13 +23,15 @@ struct StreamArgs {
     const float* slopes;
     float* lse;      // [B][H][J]: log2 of the row's sum of 2^scores (+inf: no key is seen)
     char* lo;        // [B][J][H][P]: out - round(out), 16-bit types (forward: nullptr = not wanted)
-    int2* ranges;    // [B][ceil(K / 64)]: smallest and largest document id of 64 keys
+    int4* ranges;    // [B][ceil(K / 64)]: smallest and largest document id of 64 keys, and whether some have none
     int splits;      // forward: parts the keys are split into
     float* part_o;   // splits > 1: [splits][B][H][J][P], unscaled
     float2* part_ml; // splits > 1: [splits][B][H][J]: running maximum and sum
     float* dsum;     // backward: [B][H][J] row terms dout . out
     float* dmax;     // backward, fp16: [B][H][dmax_n] largest |dout| of row groups
     int dmax_n;
+    int hparts;      // backward: parts the query heads of a key/value head are split into
+    float* part_k;   // hparts > 1: [hparts][B][G][K][dk, dv]
 };
 
 constexpr int STREAM_RANGE = 64;   // keys of one entry of `ranges`

@@ -129,29 +129,55 @@ template <typename T, int DP> struct Tile {
     }
 };
 
-// One step's rows of a tensor on their way from memory to a tile: requested
-// together, stored once the tile is free.  Rows that no query (or key) may
-// use are zeros whatever memory holds there.
-template <typename T, int DP, int ROWS> struct Stage {
+// One step's rows of a tensor, copied from memory straight into a tile:
+// buffer_load ... lds writes the 64 lanes' 16 bytes side by side, so lane l of
+// copy i takes the row and the piece that lie at that place of the tile.  The
+// buffer begins at the step's first row and ends behind its last one that
+// holds data: pieces behind the end, and behind the head size, become zeros
+// whatever memory holds there.  The copies are issued from inline assembly,
+// so that the compiler does not wait for them before the LDS reads of the
+// step at hand; copied() does, ahead of the barrier that publishes the tile.
+__device__ __forceinline__ uint32_t lds_offset(const void* p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
+}
+__device__ __forceinline__ void copy16(uint32_t lds, uint32_t voff, u32x4 rsrc) {
+    // (m0 and the descriptor may come from VALU instructions right before:
+    // five wait states to their use)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff),
+                 "s"(rsrc)
+                 : "memory");
+}
+__device__ __forceinline__ void copied() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+
+template <typename T, int DP, int ROWS> struct Copies {
     using TL = Tile<T, DP>;
     static constexpr int N = ROWS * TL::PIECES / NT;
     static_assert(ROWS * TL::PIECES % NT == 0, "pieces");
-    u32x4 x[N];
-    // ok(row): the row holds data; rows count from `base`
-    template <typename Ok, typename At>
-    __device__ __forceinline__ void load(int tid, int P, Ok ok, At at) {
+    static constexpr uint32_t NONE = 0xfffffff0u;  // behind any end
+    uint32_t vo[N];
+    uint32_t step;  // bytes between rows
+    __device__ __forceinline__ int row(int tid, int i) const { return (i * NT + tid) / TL::PIECES; }
+    __device__ __forceinline__ void init(int tid, int P, int64_t st) {
+        step = (uint32_t)(st * (int64_t)sizeof(T));
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int p = tid + i * NT, r = p / TL::PIECES, c = p % TL::PIECES;
-            x[i] = u32x4{0, 0, 0, 0};
-            if (c * TL::EPP < P && ok(r)) x[i] = *reinterpret_cast<const u32x4*>(at(r) + c * TL::EPP);
+            const int r = row(tid, i), c = (i * NT + tid) % TL::PIECES ^ swz<TL::PITCH>(r);
+            vo[i] = c * TL::EPP < P ? (uint32_t)r * step + (uint32_t)c * 16 : NONE;
         }
     }
-    __device__ __forceinline__ void store(int tid, char* t) const {
+    // rows 0 .. left - 1 from `base` into the tile at `lds`; in(r): the row may be read
+    template <typename In>
+    __device__ __forceinline__ void issue(int tid, const char* base, int left, uint32_t lds, bool all, In in) const {
+        const uint32_t n = (uint32_t)min(max(left, 0), ROWS) * step;
+        const u32x4 rsrc{uniform((uint32_t)(uintptr_t)base), uniform((uint32_t)((uintptr_t)base >> 32) & 0xffffu),
+                         uniform(n), 0x00020000u};
+        const uint32_t to = lds + (uint32_t)(tid >> 6) * 1024u;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int p = tid + i * NT;
-            *reinterpret_cast<u32x4*>(t + piece_off<TL::PITCH>(p / TL::PIECES, p % TL::PIECES)) = x[i];
+            uint32_t v = vo[i];
+            if (!all && !in(row(tid, i))) v = NONE;
+            copy16(uniform(to + (uint32_t)i * (NT * 16)), v, rsrc);
         }
     }
 };
@@ -196,8 +222,11 @@ struct Seq {
     }
 };
 
-// document ids of 64 keys: smallest and largest (an entry without any: none matches)
-__device__ __forceinline__ bool ranges_meet(int2 a, int2 b) { return a.x <= b.y && b.x <= a.y; }
+// documents of 64 keys: x the smallest id, y the largest (without any,
+// none matches), z: some of the keys are no document's
+__device__ __forceinline__ bool ranges_meet(int4 a, int2 b) { return a.x <= b.y && b.x <= a.y; }
+// all of them of one document
+__device__ __forceinline__ bool range_is(int4 a, int id) { return a.x == id && a.y == id && a.z == 0; }
 
 // 64 ids to (smallest, largest) of those that are documents
 __device__ __forceinline__ int2 wave_range(int id) {
@@ -215,8 +244,10 @@ __global__ __launch_bounds__(64) void ranges_k(StreamArgs g) {
     const int nr = (g.K + STREAM_RANGE - 1) / STREAM_RANGE, b = (int)blockIdx.x / nr, e = (int)blockIdx.x - b * nr;
     const int k = e * STREAM_RANGE + (int)threadIdx.x;
     const Seq s(g, b);
-    const int2 r = wave_range(k < s.k_len ? g.doc[(int64_t)b * g.K + k] : -1);
-    if (threadIdx.x == 0) g.ranges[(int64_t)b * nr + e] = r;
+    const int id = k < s.k_len ? g.doc[(int64_t)b * g.K + k] : -1;
+    const int2 r = wave_range(id);
+    const bool holes = __ballot(id < 0) != 0;
+    if (threadIdx.x == 0) g.ranges[(int64_t)b * nr + e] = int4{r.x, r.y, holes ? 1 : 0, 0};
 }
 
 // Block number -> (tile, head): the tiles of a head on one XCD (blocks reach
@@ -234,33 +265,32 @@ __device__ __forceinline__ void place(int nz, int& tile, int& z) {
     }
 }
 
-// Score of a lane's query and one key from the raw product: in units of log2.
-template <typename T, bool CAP>
-__device__ __forceinline__ float score(float raw, float scale2, float rcap, float cap2, float slope2, int pos, int key,
-                                       float& t) {
-    float s;
-    if constexpr (CAP) {
-        t = cap_tanh<T>(raw * rcap);
-        s = t * cap2;
-    } else {
-        s = raw * scale2;
-    }
-    return fmaf(-slope2, fabsf((float)(pos - key)), s);
-}
+// Scores of 16 N keys (or queries) of a lane from its raw products: x times
+// the returned factor, less whatever the caller adds, is the score in units
+// of log2.  dist(i): position difference of element i where a bias is wanted.
+struct Scorer {
+    float scale, rcap;  // factor of the products, or of their tanh (then of products times rcap)
+    bool bias;
+    __device__ __forceinline__ Scorer(const StreamArgs& g)
+        : scale((g.cap > 0.f ? g.cap : g.scaler) * LOG2E), rcap(g.cap > 0.f ? g.scaler / g.cap : 0.f), bias(g.slopes) {}
+    __device__ __forceinline__ float factor() const { return bias ? 1.f : scale; }
+};
 
 // ------------------------------------------------------------- forward
 // A block takes 32 WQ query rows; its waves lie WQ along the queries and
 // WK = 4 / WQ along the keys of a step (each wave 32 NS of them).
 template <typename T, int DP, bool CAP, int WQ, int NS>
-__global__ __launch_bounds__(NT) void fwd_k(StreamArgs g) {
+__global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(StreamArgs g) {
     constexpr int WK = 4 / WQ, BM = 32 * WQ, BN = 32 * WK * NS, ND = DP / 32, NC = DP / 16;
     using TL = Tile<T, DP>;
     constexpr int TB = BN * TL::PITCH;
+    // two steps' tiles where LDS holds them: one is filled while the other is read
+    constexpr int NB = 4 * TB <= 131072 ? 2 : 1;
     // joining the waves along the keys: m, l and o of all but the first
     constexpr int JOIN = WK > 1 ? (WK - 1) * 64 * (2 + 16 * ND) * 4 : 0;
-    __shared__ __attribute__((aligned(16))) char lds[(2 * TB > JOIN ? 2 * TB : JOIN) + BN * 4];
-    char *tk = lds, *tv = lds + TB;
-    int* kdoc = reinterpret_cast<int*>(lds + (2 * TB > JOIN ? 2 * TB : JOIN));
+    constexpr int TILES = 2 * NB * TB > JOIN ? 2 * NB * TB : JOIN;
+    __shared__ __attribute__((aligned(16))) char lds[TILES + 2 * BN * 4];
+    int* kdoc = reinterpret_cast<int*>(lds + TILES);
 
     const int hz = g.H / g.pack, rows = g.J * g.pack, nqt = (rows + BM - 1) / BM;
     int tile, z;
@@ -279,7 +309,7 @@ __global__ __launch_bounds__(NT) void fwd_k(StreamArgs g) {
     const int hi = live ? sq.hi(g, j) : 0, pos = sq.off + j;
     const int mydoc = g.doc && live ? sq.doc_of(g, b, j) : -1;
     const float slope2 = g.slopes && live ? g.slopes[h] * LOG2E : 0.f;
-    const float scale2 = g.scaler * LOG2E, rcap = CAP ? g.scaler / g.cap : 0.f, cap2 = g.cap * LOG2E;
+    const Scorer sc(g);
 
     Frag<T> qf[NC];
     {
@@ -297,9 +327,11 @@ __global__ __launch_bounds__(NT) void fwd_k(StreamArgs g) {
     const int hi_all = r0 < sq.q_len * g.pack ? sq.hi(g, jlast) : 0;
     const int wrow = r0 + 32 * wq, hi_low = wrow + 31 < sq.q_len * g.pack ? sq.hi(g, wrow / g.pack) : 0;
     int2 qr{0, 0};
+    int onedoc = -1;  // the document of all the wave's rows, if one
     if (g.doc) {
         __shared__ int2 wrange[4];
         const int2 r = wave_range(mydoc);
+        if (r.x == r.y && __ballot(mydoc < 0) == 0) onedoc = r.x;
         if (lane == 0) wrange[wave] = r;
         __syncthreads();
         qr = wrange[0];
@@ -331,14 +363,33 @@ __global__ __launch_bounds__(NT) void fwd_k(StreamArgs g) {
     const T* kp = reinterpret_cast<const T*>(g.k.ptr) + b * g.k.sb + kvh * g.k.sh;
     const T* vp = reinterpret_cast<const T*>(g.v.ptr) + b * g.v.sb + kvh * g.v.sh;
     const int32_t* docs = g.doc ? g.doc + (int64_t)b * g.K : nullptr;
-    Stage<T, DP, BN> sk, sv;
-    int sdoc = -1;
-    auto fetch = [&](int step) {
+    Copies<T, DP, BN> ck, cv;
+    ck.init(tid, g.P, g.k.st);
+    cv.init(tid, g.P, g.v.st);
+    const uint32_t base = lds_offset(lds);
+    // keys of a step without a hole, and of one document
+    auto whole = [&](int step, int id) {
+        bool w = true;
+#pragma unroll
+        for (int i = 0; i < BN / STREAM_RANGE; ++i) {
+            const int e = step * (BN / STREAM_RANGE) + i;
+            const int4 r = e < nr ? g.ranges[(int64_t)b * nr + e] : int4{0, 0, 1, 0};
+            w = w && (id < 0 ? r.z == 0 : range_is(r, id));
+        }
+        return w;
+    };
+    int fdoc = -1;  // documents of the step on its way, in LDS once its turn is near (put)
+    auto put = [&](int buf) {
+        if (docs && tid < BN) kdoc[buf * BN + tid] = fdoc;
+    };
+    auto fetch = [&](int step, int buf) {
         const int k0 = step * BN;
-        auto ok = [&](int r) { return k0 + r < sq.k_len && (!docs || docs[k0 + r] >= 0); };
-        sk.load(tid, g.P, ok, [&](int r) { return kp + (int64_t)(k0 + r) * g.k.st; });
-        sv.load(tid, g.P, ok, [&](int r) { return vp + (int64_t)(k0 + r) * g.v.st; });
-        if (docs && tid < BN) sdoc = k0 + tid < sq.k_len ? docs[k0 + tid] : -1;
+        if (docs && tid < BN) fdoc = k0 + tid < sq.k_len ? docs[k0 + tid] : -1;
+        const bool all = !docs || whole(step, -1);
+        auto in = [&](int r) { return k0 + r < sq.k_len && docs[k0 + r] >= 0; };
+        const uint32_t to = base + (uint32_t)(buf * 2 * TB);
+        ck.issue(tid, reinterpret_cast<const char*>(kp + (int64_t)k0 * g.k.st), sq.k_len - k0, to, all, in);
+        cv.issue(tid, reinterpret_cast<const char*>(vp + (int64_t)k0 * g.v.st), sq.k_len - k0, to + TB, all, in);
     };
 
     floatx16 o[ND];
@@ -346,84 +397,111 @@ __global__ __launch_bounds__(NT) void fwd_k(StreamArgs g) {
     for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    // m: in units of the products (or of what the bias made of them)
     float m = -INFINITY, l = 0.f;
+    const float f = sc.factor(), slack = 8.f / f;
 
     s = next(s);
-    if (s < s_end) fetch(s);
-    while (s < s_end) {
+    if (s < s_end) {
+        fetch(s, 0);
+        put(0);
+    }
+    for (int buf = 0; s < s_end; buf ^= NB - 1) {
+        copied();
         __syncthreads();
-        sk.store(tid, tk);
-        sv.store(tid, tv);
-        if (docs && tid < BN) kdoc[tid] = sdoc;
-        __syncthreads();
-        const int k0 = s * BN + 32 * NS * wk;  // this wave's keys
+        const int step = s, k0 = s * BN + 32 * NS * wk;  // this wave's keys
+        const char *tk = lds + buf * 2 * TB, *tv = tk + TB;
         s = next(s + 1);
-        if (s < s_end) fetch(s);
+        if (NB == 2 && s < s_end) fetch(s, buf ^ 1);
 
-        float x[NS][16];
+        floatx16 x[NS];
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-            floatx16 acc;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+            for (int i = 0; i < 16; ++i) x[n][i] = 0.f;
 #pragma unroll
             for (int c = 0; c < NC; ++c)
-                acc = mma<T>(TL::row(tk, 32 * (NS * wk + n) + c32, 16 * c + 8 * hh), qf[c], acc);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[n][i] = acc[i];
+                x[n] = mma<T>(TL::row(tk, 32 * (NS * wk + n) + c32, 16 * c + 8 * hh), qf[c], x[n]);
         }
-        float t;
+        if constexpr (CAP) {
 #pragma unroll
-        for (int n = 0; n < NS; ++n)
+            for (int n = 0; n < NS; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                x[n][i] = score<T, CAP>(x[n][i], scale2, rcap, cap2, slope2, pos,
-                                        k0 + 32 * n + 8 * (i >> 2) + 4 * hh + (i & 3), t);
-        if (k0 + 32 * NS > hi_low || docs) {
+                for (int i = 0; i < 16; ++i) x[n][i] = cap_tanh<T>(x[n][i] * sc.rcap);
+        }
+        if (sc.bias) {
+            const float far = (float)(pos - k0 - 4 * hh);
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    x[n][i] = fmaf(-slope2, fabsf(far - (float)(32 * n + 8 * (i >> 2) + (i & 3))), x[n][i] * sc.scale);
+        }
+        if (docs && !(onedoc >= 0 && whole(step, onedoc))) {
 #pragma unroll
             for (int n = 0; n < NS; ++n)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int kk = 32 * n + 8 * q + 4 * hh;
-                    int4 kd{mydoc, mydoc, mydoc, mydoc};
-                    if (docs) kd = *reinterpret_cast<const int4*>(kdoc + 32 * NS * wk + kk);
+                    const int4 kd = *reinterpret_cast<const int4*>(kdoc + buf * BN + 32 * (NS * wk + n) + 8 * q + 4 * hh);
                     const int id[4] = {kd.x, kd.y, kd.z, kd.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (k0 + kk + i >= hi || (docs && (id[i] != mydoc || mydoc < 0))) x[n][4 * q + i] = -INFINITY;
+                        if (id[i] != mydoc || mydoc < 0) x[n][4 * q + i] = -INFINITY;
                 }
         }
-        float mx = x[0][0];
+        if (k0 + 32 * NS > hi_low) {
+            const int end = hi - k0 - 4 * hh;
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (32 * n + 8 * (i >> 2) + (i & 3) >= end) x[n][i] = -INFINITY;
+        }
+        float mx = -INFINITY;
 #pragma unroll
         for (int n = 0; n < NS; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[n][i]);
-        mx = fmaxf(m, fmaxf(mx, other_half(mx)));
-        const float ms = mx == -INFINITY ? 0.f : mx;
-        const float alpha = __builtin_amdgcn_exp2f(m - ms);
-        m = mx;
-        l *= alpha;
+            for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, x[n][i]), x[n][i + 1]);
+        mx = fmaxf(mx, other_half(mx));
+        // the row's reference value follows its maximum only once that is 2^8
+        // above it: until then sums and products stay far inside their types
+        if (__any(mx > m + slack)) {
+            const float mn = fmaxf(m, mx);
+            const float alpha = mn == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * f);
+            m = mn;
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+        }
+        const float mf = m == -INFINITY ? 0.f : -m * f;
+        float p[NS][16];
 #pragma unroll
         for (int n = 0; n < NS; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                x[n][i] = __builtin_amdgcn_exp2f(x[n][i] - ms);
-                l += x[n][i];
+                p[n][i] = __builtin_amdgcn_exp2f(fmaf(x[n][i], f, mf));
+                l += p[n][i];
             }
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
 #pragma unroll
         for (int n = 0; n < NS; ++n)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const Frag<T> p = frag_acc<T>(&x[n][8 * c]);
+                const Frag<T> pf = frag_acc<T>(&p[n][8 * c]);
 #pragma unroll
                 for (int d = 0; d < ND; ++d)
-                    o[d] = mma<T>(TL::col(tv, 32 * (NS * wk + n) + 16 * c, 32 * d, lane), p, o[d]);
+                    o[d] = mma<T>(TL::col(tv, 32 * (NS * wk + n) + 16 * c, 32 * d, lane), pf, o[d]);
             }
+        if (NB == 2) {
+            put(buf ^ 1);
+        } else {
+            __syncthreads();
+            if (s < s_end) fetch(s, 0);
+            put(0);
+        }
     }
+    m *= f;  // from here in units of log2
     l += other_half(l);
 
     if constexpr (WK > 1) {
@@ -597,24 +675,34 @@ __device__ __forceinline__ Gain gain(const StreamArgs& g, int b, int kvh) {
     const int e = top > 0.f && top < INFINITY ? -ilogbf(top) : 0;
     return Gain{10.f, 1.f / 1024.f, ldexpf(1.f, e - 10), ldexpf(1.f, -e)};
 }
-template <typename T> __device__ __forceinline__ float held(float x) {
-    if constexpr (__is_same(T, half_t)) return x > 65504.f ? 65504.f : x < -65504.f ? -65504.f : x;  // (NaN stays)
-    return x;
+// p (dout . v - D), scaled
+template <typename T> __device__ __forceinline__ float score_grad(float p, float dpd, const Gain& gn) {
+    if constexpr (__is_same(T, half_t)) return p * dpd * gn.ds;
+    return p * dpd;
+}
+// fp16: conversions to the type that pass its largest value give that value
+// instead of an infinity (infinities and NaN stay): bit 23 of the mode
+// register, while score gradients are formed
+template <typename T> __device__ __forceinline__ void hold_overflow(bool on) {
+    if constexpr (__is_same(T, half_t)) __builtin_amdgcn_s_setreg((23 << 6) | 1, on ? 1 : 0);
 }
 
 // dK and dV of 128 keys (32 a wave) of one key/value head: walks the query
-// rows of all its query heads, 64 a step.
+// rows of its query heads (of a part of them where the heads are split),
+// 64 a step.
 template <typename T, int DP, bool CAP>
-__global__ __launch_bounds__(NT) void dkv_k(StreamArgs g) {
+__global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k(StreamArgs g) {
     constexpr int BQ = 64, ND = DP / 32, NC = DP / 16;
     using TL = Tile<T, DP>;
     constexpr int TB = BQ * TL::PITCH;
-    __shared__ __attribute__((aligned(16))) char lds[2 * TB];
-    __shared__ __attribute__((aligned(16))) float row_lse[BQ], row_d[BQ];
-    __shared__ __attribute__((aligned(16))) int row_hi[BQ], row_doc[BQ];
-    char *tq = lds, *td = lds + TB;
+    // tiles of q and dout, and the rows' numbers: -lse, -D, bounds, documents
+    constexpr int STEP = 2 * TB + BQ * 16;
+    constexpr int NB = 2 * STEP <= 131072 + 4096 ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) char lds[NB * STEP];
     int tile, z;
-    place(g.B * g.G, tile, z);
+    place(g.B * g.G * g.hparts, tile, z);
+    const int part = z % g.hparts;
+    z /= g.hparts;
     const int b = z / g.G, kvh = z - b * g.G, grp = g.H / g.G, k0 = tile * STREAM_KEYS;
     const int tid = threadIdx.x, lane = tid & 63, c32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -623,7 +711,7 @@ __global__ __launch_bounds__(NT) void dkv_k(StreamArgs g) {
     const int key = k0 + 32 * wave + c32;
     const int kd = docs ? (key < sq.k_len ? docs[key] : -1) : 0;
     const bool kin = key < sq.k_len && kd >= 0;
-    const float scale2 = g.scaler * LOG2E, rcap = CAP ? g.scaler / g.cap : 0.f, cap2 = g.cap * LOG2E;
+    const Scorer sc(g);
     const Gain gn = gain<T>(g, b, kvh);
 
     Frag<T> kf[NC], vf[NC];
@@ -649,105 +737,146 @@ __global__ __launch_bounds__(NT) void dkv_k(StreamArgs g) {
     const int nst = k0 < sq.k_len ? (sq.q_len + BQ - 1) / BQ : 0;
     const int nr = (g.K + STREAM_RANGE - 1) / STREAM_RANGE;
     int2 kr{0, 0};
+    int onedoc = -1;  // the document of all the wave's keys, if one
     if (docs) {
         kr = int2{INT32_MAX, -1};
 #pragma unroll
         for (int i = 0; i < STREAM_KEYS / STREAM_RANGE; ++i) {
             const int e = k0 / STREAM_RANGE + i;
             if (e < nr) {
-                const int2 r = g.ranges[(int64_t)b * nr + e];
+                const int4 r = g.ranges[(int64_t)b * nr + e];
                 kr = int2{min(kr.x, r.x), max(kr.y, r.y)};
+                if (i == 32 * wave / STREAM_RANGE && r.x == r.y && r.z == 0) onedoc = r.x;
             }
         }
     }
+    // the step's rows lie in at most two entries
+    auto entry = [&](int step, int i) {
+        const int p = sq.off + step * BQ + i * (BQ - 1), e = max(p, 0) / STREAM_RANGE;
+        return p >= 0 && e < nr ? g.ranges[(int64_t)b * nr + e] : int4{INT32_MAX, -1, 1, 0};
+    };
     auto next = [&](int from) {
         if (!docs) return from;
         for (; from < nst; from += 64) {
-            bool in = false;
-            if (from + lane < nst) {
-                // the step's rows lie in at most two entries
-                const int p = sq.off + (from + lane) * BQ, e0 = max(p, 0) / STREAM_RANGE;
-                const int e1 = max(p + BQ - 1, 0) / STREAM_RANGE;
-                if (e0 < nr) in |= ranges_meet(g.ranges[(int64_t)b * nr + e0], kr);
-                if (e1 < nr) in |= ranges_meet(g.ranges[(int64_t)b * nr + e1], kr);
-            }
+            const bool in = from + lane < nst &&
+                            (ranges_meet(entry(from + lane, 0), kr) || ranges_meet(entry(from + lane, 1), kr));
             const uint64_t mk = __ballot(in);
             if (mk) return from + (int)__builtin_ctzll(mk);
         }
         return nst;
     };
 
-    for (int hg = 0; hg < grp; ++hg) {
+    Copies<T, DP, BQ> cq, cd;
+    cq.init(tid, g.P, g.q.st);
+    cd.init(tid, g.P, g.dout.st);
+    const uint32_t base = lds_offset(lds);
+    auto rows_of = [&](int buf) { return reinterpret_cast<float*>(lds + buf * STEP + 2 * TB); };
+    hold_overflow<T>(true);
+    const int h_end = min(grp, (part + 1) * ((grp + g.hparts - 1) / g.hparts));
+    for (int hg = part * ((grp + g.hparts - 1) / g.hparts); hg < h_end; ++hg) {
         const int h = kvh * grp + hg;
         const float slope2 = g.slopes ? g.slopes[h] * LOG2E : 0.f;
         const T* qp = reinterpret_cast<const T*>(g.q.ptr) + b * g.q.sb + h * g.q.sh;
         const T* dp = reinterpret_cast<const T*>(g.dout.ptr) + b * g.dout.sb + h * g.dout.sh;
         const int64_t zr = ((int64_t)b * g.H + h) * g.J;
-        Stage<T, DP, BQ> st_q, st_d;
-        float f_lse = INFINITY, f_d = 0.f;
-        int f_hi = 0, f_doc = -1;
-        auto fetch = [&](int step) {
+        float f_lse = 0.f, f_d = 0.f;  // the step on its way: its rows' numbers, in LDS once its turn is near
+        int f_hi = 0, f_doc = 0;
+        auto put = [&](int buf) {
+            if (tid < BQ) {
+                float* r = rows_of(buf) + tid;
+                r[0] = f_lse;
+                r[BQ] = f_d;
+                reinterpret_cast<int*>(r)[2 * BQ] = f_hi;
+                reinterpret_cast<int*>(r)[3 * BQ] = f_doc;
+            }
+        };
+        auto fetch = [&](int step, int buf) {
             const int j0 = step * BQ;
-            auto ok = [&](int r) { return j0 + r < sq.q_len && (!docs || sq.doc_of(g, b, j0 + r) >= 0); };
-            st_q.load(tid, g.P, ok, [&](int r) { return qp + (int64_t)(j0 + r) * g.q.st; });
-            st_d.load(tid, g.P, ok, [&](int r) { return dp + (int64_t)(j0 + r) * g.dout.st; });
+            const bool all = !docs || (entry(step, 0).z == 0 && entry(step, 1).z == 0);
+            auto in = [&](int r) { return sq.doc_of(g, b, j0 + r) >= 0; };
             if (tid < BQ) {
                 const int j = j0 + tid;
-                const bool in = j < sq.q_len;
-                f_lse = in ? g.lse[zr + j] : INFINITY;
-                f_d = in ? g.dsum[zr + j] : 0.f;
+                const bool row = j < sq.q_len;
+                f_lse = row ? gn.p2 - g.lse[zr + j] : -INFINITY;
+                f_d = row ? -g.dsum[zr + j] : 0.f;
                 f_hi = sq.hi(g, j);
                 f_doc = docs ? sq.doc_of(g, b, j) : 0;
             }
+            const uint32_t to = base + (uint32_t)(buf * STEP);
+            cq.issue(tid, reinterpret_cast<const char*>(qp + (int64_t)j0 * g.q.st), sq.q_len - j0, to, all, in);
+            cd.issue(tid, reinterpret_cast<const char*>(dp + (int64_t)j0 * g.dout.st), sq.q_len - j0, to + TB, all, in);
         };
         int s = next(first);
-        if (s < nst) fetch(s);
-        while (s < nst) {
+        __syncthreads();  // (the last head's last step has been read)
+        if (s < nst) {
+            fetch(s, 0);
+            put(0);
+        }
+        for (int buf = 0; s < nst; buf ^= NB - 1) {
+            copied();
             __syncthreads();
-            st_q.store(tid, tq);
-            st_d.store(tid, td);
-            if (tid < BQ) {
-                row_lse[tid] = f_lse - gn.p2;
-                row_d[tid] = f_d;
-                row_hi[tid] = f_hi;
-                row_doc[tid] = f_doc;
-            }
-            __syncthreads();
-            const int j0 = s * BQ;
+            const int step = s, j0 = s * BQ;
+            const char *tq = lds + buf * STEP, *td = tq + TB;
+            const float* rows = rows_of(buf);
             s = next(s + 1);
-            if (s < nst) fetch(s);
-
+            if (NB == 2 && s < nst) fetch(s, buf ^ 1);
+            // (rows behind the last query have zeros and no probabilities)
+            const bool bound = k0 + 32 * wave + 32 > sq.hi(g, j0);
+            const bool other = docs && !(onedoc >= 0 && range_is(entry(step, 0), onedoc) &&
+                                         range_is(entry(step, 1), onedoc));
 #pragma unroll
             for (int n = 0; n < BQ / 32; ++n) {
-                floatx16 sc, dpv;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sc[i] = dpv[i] = 0.f;
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    sc = mma<T>(TL::row(tq, 32 * n + c32, 16 * c + 8 * hh), kf[c], sc);
-                    dpv = mma<T>(TL::row(td, 32 * n + c32, 16 * c + 8 * hh), vf[c], dpv);
-                }
-                float p[16], ds[16];
+                floatx16 x, dpd;
+                float nl[16];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int r = 32 * n + 8 * q + 4 * hh;
-                    const floatx4 ls = *reinterpret_cast<const floatx4*>(row_lse + r);
-                    const floatx4 dd = *reinterpret_cast<const floatx4*>(row_d + r);
-                    const int4 rh = *reinterpret_cast<const int4*>(row_hi + r);
-                    const int4 rd = *reinterpret_cast<const int4*>(row_doc + r);
-                    const int hi4[4] = {rh.x, rh.y, rh.z, rh.w}, id4[4] = {rd.x, rd.y, rd.z, rd.w};
+                    const floatx4 a = *reinterpret_cast<const floatx4*>(rows + 32 * n + 8 * q + 4 * hh);
+                    const floatx4 d = *reinterpret_cast<const floatx4*>(rows + BQ + 32 * n + 8 * q + 4 * hh);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int a = 4 * q + i;
-                        float t = 0.f;
-                        const float x = score<T, CAP>(sc[a], scale2, rcap, cap2, slope2, sq.off + j0 + r + i, key, t);
-                        const bool see = key < hi4[i] && kin && id4[i] == kd;
-                        p[a] = see ? __builtin_amdgcn_exp2f(x - ls[i]) : 0.f;
-                        float y = p[a] * (dpv[a] - dd[i]) * gn.ds;
-                        if constexpr (CAP) y *= 1.f - t * t;
-                        ds[a] = see ? held<T>(y) : 0.f;
+                        x[4 * q + i] = 0.f;
+                        nl[4 * q + i] = a[i];
+                        dpd[4 * q + i] = d[i];  // dout . v - D
                     }
                 }
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    x = mma<T>(TL::row(tq, 32 * n + c32, 16 * c + 8 * hh), kf[c], x);
+                    dpd = mma<T>(TL::row(td, 32 * n + c32, 16 * c + 8 * hh), vf[c], dpd);
+                }
+                float p[16], ds[16];
+                if constexpr (CAP) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        x[i] = cap_tanh<T>(x[i] * sc.rcap);
+                        dpd[i] *= 1.f - x[i] * x[i];
+                    }
+                }
+                if (sc.bias) {
+                    const float far = (float)(sq.off + j0 + 32 * n + 4 * hh - key);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        p[i] = fmaf(-slope2, fabsf(far + (float)(8 * (i >> 2) + (i & 3))), fmaf(x[i], sc.scale, nl[i]));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) p[i] = fmaf(x[i], sc.scale, nl[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]);
+                if (bound || other) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int* r = reinterpret_cast<const int*>(rows) + 2 * BQ + 32 * n + 8 * q + 4 * hh;
+                        const int4 rh = *reinterpret_cast<const int4*>(r);
+                        const int4 rd = *reinterpret_cast<const int4*>(r + BQ);
+                        const int hi4[4] = {rh.x, rh.y, rh.z, rh.w}, id4[4] = {rd.x, rd.y, rd.z, rd.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (key >= hi4[i] || id4[i] != kd || !kin) p[4 * q + i] = 0.f;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) ds[i] = score_grad<T>(p[i], dpd[i], gn);
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const Frag<T> pf = frag_acc<T>(p + 8 * c), sf = frag_acc<T>(ds + 8 * c);
@@ -758,12 +887,21 @@ __global__ __launch_bounds__(NT) void dkv_k(StreamArgs g) {
                     }
                 }
             }
+            if (NB == 2) {
+                put(buf ^ 1);
+            } else {
+                __syncthreads();
+                if (s < nst) fetch(s, 0);
+                put(0);
+            }
         }
     }
     if (key >= g.K) return;
+    hold_overflow<T>(false);
+    const float fk = g.scaler * gn.dsinv;
     T* dkp = reinterpret_cast<T*>(g.dk.ptr) + b * g.dk.sb + kvh * g.dk.sh + (int64_t)key * g.dk.st;
     T* dvp = reinterpret_cast<T*>(g.dv.ptr) + b * g.dv.sb + kvh * g.dv.sh + (int64_t)key * g.dv.st;
-    const float fk = g.scaler * gn.dsinv;
+    float* pk = g.part_k + ((((int64_t)part * g.B + b) * g.G + kvh) * g.K + key) * 2 * g.P;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -776,22 +914,45 @@ __global__ __launch_bounds__(NT) void dkv_k(StreamArgs g) {
                 y[i] = dk[d][4 * q + i] * fk;
                 w[i] = dv[d][4 * q + i] * gn.pinv;
             }
-            store4<T>(dkp + e, y);
-            store4<T>(dvp + e, w);
+            if (g.hparts > 1) {
+                store4<float>(pk + e, y);
+                store4<float>(pk + g.P + e, w);
+            } else {
+                store4<T>(dkp + e, y);
+                store4<T>(dvp + e, w);
+            }
         }
+}
+
+// Sums of the head parts' dK and dV, in their order: 8 elements a thread.
+template <typename T>
+__global__ __launch_bounds__(NT) void dkv_join_k(StreamArgs g) {
+    const int np = 2 * g.P / 8;
+    const int64_t rows = (int64_t)g.B * g.G * g.K, at = (int64_t)blockIdx.x * NT + threadIdx.x, row = at / np;
+    if (row >= rows) return;
+    const int e = (int)(at - row * np) * 8;
+    float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < g.hparts; ++s) {
+        float x[8];
+        V8<float>::load(g.part_k + (s * rows + row) * 2 * g.P + e, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] += x[i];
+    }
+    const int key = (int)(row % g.K), kvh = (int)(row / g.K % g.G), b = (int)(row / g.K / g.G);
+    const StreamRows& to = e < g.P ? g.dk : g.dv;
+    V8<T>::store(reinterpret_cast<T*>(to.ptr) + b * to.sb + kvh * to.sh + (int64_t)key * to.st + (e < g.P ? e : e - g.P), y);
 }
 
 // dQ of 128 query rows (32 a wave) of one head: walks their keys as the
 // forward does.
 template <typename T, int DP, bool CAP>
-__global__ __launch_bounds__(NT) void dq_k(StreamArgs g) {
+__global__ __launch_bounds__(NT, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void dq_k(StreamArgs g) {
     constexpr int BM = 128, BN = 64, NS = 2, ND = DP / 32, NC = DP / 16;
     using TL = Tile<T, DP>;
-    constexpr int TB = BN * TL::PITCH;
-    __shared__ __attribute__((aligned(16))) char lds[2 * TB];
-    __shared__ __attribute__((aligned(16))) int kdoc[BN];
+    constexpr int TB = BN * TL::PITCH, NB = 4 * TB <= 131072 ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) char lds[2 * NB * TB];
+    __shared__ __attribute__((aligned(16))) int kdoc[2 * BN];
     __shared__ int2 wrange[4];
-    char *tk = lds, *tv = lds + TB;
     const int nqt = (g.J + BM - 1) / BM;
     int tile, z;
     place(g.B * g.H, tile, z);
@@ -806,10 +967,10 @@ __global__ __launch_bounds__(NT) void dq_k(StreamArgs g) {
     const bool live = j < sq.q_len && mydoc >= 0;
     const int hi = live ? sq.hi(g, j) : 0;
     const float slope2 = g.slopes ? g.slopes[h] * LOG2E : 0.f;
-    const float scale2 = g.scaler * LOG2E, rcap = CAP ? g.scaler / g.cap : 0.f, cap2 = g.cap * LOG2E;
+    const Scorer sc(g);
     const Gain gn = gain<T>(g, b, kvh);
     const int64_t zr = ((int64_t)b * g.H + h) * g.J + j;
-    const float lse = live ? g.lse[zr] - gn.p2 : INFINITY, dd = live ? g.dsum[zr] : 0.f;
+    const float nl = live ? gn.p2 - g.lse[zr] : -INFINITY, nd = live ? -g.dsum[zr] : 0.f;
 
     Frag<T> qf[NC], df[NC];
     {
@@ -822,11 +983,14 @@ __global__ __launch_bounds__(NT) void dq_k(StreamArgs g) {
             df[c] = live && e < g.P ? frag_load<T>(dp + e) : frag_zero<T>();
         }
     }
-    const int jlast = min(min(j0 + BM, g.J), sq.q_len) - 1;
+    const int jlast = min(min(j0 + BM, g.J), sq.q_len) - 1, wj = j0 + 32 * wave;
     const int steps = j0 < sq.q_len ? (sq.hi(g, jlast) + BN - 1) / BN : 0;
+    const int hi_low = wj + 31 < sq.q_len ? sq.hi(g, wj) : 0;
     int2 qr{0, 0};
+    int onedoc = -1;
     if (docs) {
         const int2 r = wave_range(mydoc);
+        if (r.x == r.y && __ballot(mydoc < 0) == 0) onedoc = r.x;
         if (lane == 0) wrange[wave] = r;
         __syncthreads();
         qr = wrange[0];
@@ -834,10 +998,11 @@ __global__ __launch_bounds__(NT) void dq_k(StreamArgs g) {
         for (int w = 1; w < 4; ++w) qr = int2{min(qr.x, wrange[w].x), max(qr.y, wrange[w].y)};
     }
     const int nr = (g.K + STREAM_RANGE - 1) / STREAM_RANGE;
+    const int4* ranges = g.ranges + (int64_t)b * nr;
     auto next = [&](int from) {
         if (!docs) return from;
         for (; from < steps; from += 64) {
-            const bool in = from + lane < steps && ranges_meet(g.ranges[(int64_t)b * nr + from + lane], qr);
+            const bool in = from + lane < steps && ranges_meet(ranges[from + lane], qr);
             const uint64_t mk = __ballot(in);
             if (mk) return from + (int)__builtin_ctzll(mk);
         }
@@ -845,14 +1010,22 @@ __global__ __launch_bounds__(NT) void dq_k(StreamArgs g) {
     };
     const T* kp = reinterpret_cast<const T*>(g.k.ptr) + b * g.k.sb + kvh * g.k.sh;
     const T* vp = reinterpret_cast<const T*>(g.v.ptr) + b * g.v.sb + kvh * g.v.sh;
-    Stage<T, DP, BN> sk, sv;
-    int sdoc = -1;
-    auto fetch = [&](int step) {
+    Copies<T, DP, BN> ck, cv;
+    ck.init(tid, g.P, g.k.st);
+    cv.init(tid, g.P, g.v.st);
+    const uint32_t base = lds_offset(lds);
+    int fdoc = -1;
+    auto put = [&](int buf) {
+        if (docs && tid < BN) kdoc[buf * BN + tid] = fdoc;
+    };
+    auto fetch = [&](int step, int buf) {
         const int k0 = step * BN;
-        auto ok = [&](int r) { return k0 + r < sq.k_len && (!docs || docs[k0 + r] >= 0); };
-        sk.load(tid, g.P, ok, [&](int r) { return kp + (int64_t)(k0 + r) * g.k.st; });
-        sv.load(tid, g.P, ok, [&](int r) { return vp + (int64_t)(k0 + r) * g.v.st; });
-        if (docs && tid < BN) sdoc = k0 + tid < sq.k_len ? docs[k0 + tid] : -1;
+        if (docs && tid < BN) fdoc = k0 + tid < sq.k_len ? docs[k0 + tid] : -1;
+        const bool all = !docs || ranges[step].z == 0;
+        auto in = [&](int r) { return k0 + r < sq.k_len && docs[k0 + r] >= 0; };
+        const uint32_t to = base + (uint32_t)(buf * 2 * TB);
+        ck.issue(tid, reinterpret_cast<const char*>(kp + (int64_t)k0 * g.k.st), sq.k_len - k0, to, all, in);
+        cv.issue(tid, reinterpret_cast<const char*>(vp + (int64_t)k0 * g.v.st), sq.k_len - k0, to + TB, all, in);
     };
     floatx16 dq[ND];
 #pragma unroll
@@ -861,44 +1034,69 @@ __global__ __launch_bounds__(NT) void dq_k(StreamArgs g) {
         for (int i = 0; i < 16; ++i) dq[d][i] = 0.f;
 
     int s = next(0);
-    if (s < steps) fetch(s);
-    while (s < steps) {
-        __syncthreads();
-        sk.store(tid, tk);
-        sv.store(tid, tv);
-        if (docs && tid < BN) kdoc[tid] = sdoc;
+    if (s < steps) {
+        fetch(s, 0);
+        put(0);
+    }
+    hold_overflow<T>(true);
+    for (int buf = 0; s < steps; buf ^= NB - 1) {
+        copied();
         __syncthreads();
         const int k0 = s * BN;
+        const char *tk = lds + buf * 2 * TB, *tv = tk + TB;
+        const bool other = docs && !(onedoc >= 0 && range_is(ranges[s], onedoc));
         s = next(s + 1);
-        if (s < steps) fetch(s);
+        if (NB == 2 && s < steps) fetch(s, buf ^ 1);
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-            floatx16 sc, dpv;
+            floatx16 x, dpd;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[i] = dpv[i] = 0.f;
+            for (int i = 0; i < 16; ++i) {
+                x[i] = 0.f;
+                dpd[i] = nd;  // dout . v - D
+            }
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                sc = mma<T>(TL::row(tk, 32 * n + c32, 16 * c + 8 * hh), qf[c], sc);
-                dpv = mma<T>(TL::row(tv, 32 * n + c32, 16 * c + 8 * hh), df[c], dpv);
+                x = mma<T>(TL::row(tk, 32 * n + c32, 16 * c + 8 * hh), qf[c], x);
+                dpd = mma<T>(TL::row(tv, 32 * n + c32, 16 * c + 8 * hh), df[c], dpd);
             }
-            float ds[16];
+            float p[16], ds[16];
+            if constexpr (CAP) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int kk = 32 * n + 8 * q + 4 * hh;
-                int4 kd{mydoc, mydoc, mydoc, mydoc};
-                if (docs) kd = *reinterpret_cast<const int4*>(kdoc + kk);
-                const int id[4] = {kd.x, kd.y, kd.z, kd.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int a = 4 * q + i;
-                    float t = 0.f;
-                    const float x = score<T, CAP>(sc[a], scale2, rcap, cap2, slope2, pos, k0 + kk + i, t);
-                    const bool see = k0 + kk + i < hi && id[i] == mydoc;
-                    float y = __builtin_amdgcn_exp2f(x - lse) * (dpv[a] - dd) * gn.ds;
-                    if constexpr (CAP) y *= 1.f - t * t;
-                    ds[a] = see ? held<T>(y) : 0.f;
+                for (int i = 0; i < 16; ++i) {
+                    x[i] = cap_tanh<T>(x[i] * sc.rcap);
+                    dpd[i] *= 1.f - x[i] * x[i];
                 }
             }
+            if (sc.bias) {
+                const float far = (float)(pos - k0 - 32 * n - 4 * hh);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    p[i] = fmaf(-slope2, fabsf(far - (float)(8 * (i >> 2) + (i & 3))), fmaf(x[i], sc.scale, nl));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) p[i] = fmaf(x[i], sc.scale, nl);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]);
+            if (other) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int4 kd = *reinterpret_cast<const int4*>(kdoc + buf * BN + 32 * n + 8 * q + 4 * hh);
+                    const int id[4] = {kd.x, kd.y, kd.z, kd.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (id[i] != mydoc) p[4 * q + i] = 0.f;
+                }
+            }
+            if (k0 + BN > hi_low) {
+                const int end = hi - k0 - 32 * n - 4 * hh;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (8 * (i >> 2) + (i & 3) >= end) p[i] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ds[i] = score_grad<T>(p[i], dpd[i], gn);
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const Frag<T> sf = frag_acc<T>(ds + 8 * c);
@@ -906,8 +1104,16 @@ __global__ __launch_bounds__(NT) void dq_k(StreamArgs g) {
                 for (int d = 0; d < ND; ++d) dq[d] = mma<T>(TL::col(tk, 32 * n + 16 * c, 32 * d, lane), sf, dq[d]);
             }
         }
+        if (NB == 2) {
+            put(buf ^ 1);
+        } else {
+            __syncthreads();
+            if (s < steps) fetch(s, 0);
+            put(0);
+        }
     }
     if (j >= g.J) return;
+    hold_overflow<T>(false);
     T* dqp = reinterpret_cast<T*>(g.dq.ptr) + b * g.dq.sb + h * g.dq.sh + (int64_t)j * g.dq.st;
     const float f = g.scaler * gn.dsinv;
 #pragma unroll
@@ -935,7 +1141,11 @@ template <typename T, int DP, bool CAP> void launch_fwd(const StreamArgs& a, boo
 template <typename T, int DP, bool CAP> void launch_bwd(const StreamArgs& a, hipStream_t st) {
     const int64_t nk = (int64_t)((a.K + STREAM_KEYS - 1) / STREAM_KEYS) * a.B * a.G;
     const int64_t nq = (int64_t)((a.J + 127) / 128) * a.B * a.H;
-    if (nk > 0) dkv_k<T, DP, CAP><<<dim3((unsigned)nk), NT, 0, st>>>(a);
+    if (nk > 0) dkv_k<T, DP, CAP><<<dim3((unsigned)(nk * a.hparts)), NT, 0, st>>>(a);
+    if (nk > 0 && a.hparts > 1) {
+        const int64_t n = (int64_t)a.B * a.G * a.K * (2 * a.P / 8);
+        dkv_join_k<T><<<dim3((unsigned)((n + NT - 1) / NT)), NT, 0, st>>>(a);
+    }
     if (nq > 0) dq_k<T, DP, CAP><<<dim3((unsigned)nq), NT, 0, st>>>(a);
 }
 
