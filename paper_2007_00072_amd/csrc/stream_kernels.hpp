@@ -20,6 +20,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 #include "stream.hpp"
 
 namespace dm {
@@ -191,14 +193,33 @@ template <typename T> __device__ __forceinline__ void store4(T* p, const float* 
 // the other lane half's value
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
 
-// tanh for the capped scores: from one exponential in the 16-bit types
-// (absolute error about 1e-7, far under their resolution), the library's in
-// float32
-template <typename T> __device__ __forceinline__ float cap_tanh(float x) {
-    if constexpr (sizeof(T) == 2)
-        return 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * LOG2E)) + 1.f);
-    return tanhf(x);
-}
+// Raw products to scores.  With x the returned value, a score in units of
+// log2 is factor x + offset - what the bias takes, and the same for all of a
+// row but for x, so that the offset only matters where lse does.
+// Capped scores: the 16-bit types take t = tanh z = 1 - 2 u, u = 1 / (e^2z + 1),
+// by one exponential and one reciprocal (absolute error about 1e-7, far
+// under their resolution) and go on with x = -u: no instruction makes t, and
+// 1 - t^2 = 4 (u - u^2) in the backward.  float32 takes the library's tanh.
+template <typename T, bool CAP, bool BIAS> struct Scorer {
+    static constexpr bool U = CAP && sizeof(T) == 2;
+    float zc, scale, offset;  // z (or its exponent's argument) per product; log2 units per x
+    __device__ __forceinline__ Scorer(const StreamArgs& g) {
+        zc = CAP ? g.scaler / g.cap * (U ? 2.f * LOG2E : 1.f) : 0.f;
+        scale = (CAP ? g.cap * (U ? 2.f : 1.f) : g.scaler) * LOG2E;
+        offset = U ? g.cap * LOG2E : 0.f;
+    }
+    __device__ __forceinline__ float value(float raw) const {
+        if constexpr (U) return -__builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(raw * zc) + 1.f);
+        if constexpr (CAP) return tanhf(raw * zc);
+        return raw;
+    }
+    // 1 - t^2, less the factor SLOPE
+    static constexpr float SLOPE = U ? 4.f : 1.f;
+    __device__ __forceinline__ static float slope(float x) {
+        if constexpr (U) return fmaf(-x, x, -x);
+        return fmaf(-x, x, 1.f);
+    }
+};
 
 // Which keys a query sees.  A causal query at position p sees keys 0 .. p,
 // and keys below the sequence's prefix: all keys below `hi`, of which its
@@ -250,6 +271,16 @@ __global__ __launch_bounds__(64) void ranges_k(StreamArgs g) {
     if (threadIdx.x == 0) g.ranges[(int64_t)b * nr + e] = int4{r.x, r.y, holes ? 1 : 0, 0};
 }
 
+// Which of 64 steps a block walks, and how: bits for step `base` + i.  The
+// entries behind a step's keys (or rows) are read once for the 64.
+struct Window {
+    int base;
+    uint64_t meet;   // some of it may be of the block's documents
+    uint64_t holes;  // some of it is of none: copied row by row
+    uint64_t whole;  // all of it is of the one document of this wave's rows (keys)
+    __device__ __forceinline__ bool is(uint64_t m, int step) const { return (m >> (step - base)) & 1; }
+};
+
 // Block number -> (tile, head): the tiles of a head on one XCD (blocks reach
 // the 8 XCDs in turn), so that its L2 serves the rows they share; all heads'
 // first tiles before the second ones.
@@ -265,21 +296,10 @@ __device__ __forceinline__ void place(int nz, int& tile, int& z) {
     }
 }
 
-// Scores of 16 N keys (or queries) of a lane from its raw products: x times
-// the returned factor, less whatever the caller adds, is the score in units
-// of log2.  dist(i): position difference of element i where a bias is wanted.
-struct Scorer {
-    float scale, rcap;  // factor of the products, or of their tanh (then of products times rcap)
-    bool bias;
-    __device__ __forceinline__ Scorer(const StreamArgs& g)
-        : scale((g.cap > 0.f ? g.cap : g.scaler) * LOG2E), rcap(g.cap > 0.f ? g.scaler / g.cap : 0.f), bias(g.slopes) {}
-    __device__ __forceinline__ float factor() const { return bias ? 1.f : scale; }
-};
-
 // ------------------------------------------------------------- forward
 // A block takes 32 WQ query rows; its waves lie WQ along the queries and
 // WK = 4 / WQ along the keys of a step (each wave 32 NS of them).
-template <typename T, int DP, bool CAP, int WQ, int NS>
+template <typename T, int DP, bool CAP, bool BIAS, int WQ, int NS>
 __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(StreamArgs g) {
     constexpr int WK = 4 / WQ, BM = 32 * WQ, BN = 32 * WK * NS, ND = DP / 32, NC = DP / 16;
     using TL = Tile<T, DP>;
@@ -306,10 +326,11 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
     const int r0 = tile * BM, row = r0 + 32 * wq + c32;  // this lane's query row
     const int j = row / g.pack, h = h0 + row - j * g.pack;
     const bool live = row < rows && j < sq.q_len;
-    const int hi = live ? sq.hi(g, j) : 0, pos = sq.off + j;
+    const int pos = sq.off + j;
     const int mydoc = g.doc && live ? sq.doc_of(g, b, j) : -1;
+    const int hi = live && !(g.doc && mydoc < 0) ? sq.hi(g, j) : 0;
     const float slope2 = g.slopes && live ? g.slopes[h] * LOG2E : 0.f;
-    const Scorer sc(g);
+    const Scorer<T, CAP, BIAS> sc(g);
 
     Frag<T> qf[NC];
     {
@@ -317,7 +338,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int e = 16 * c + 8 * hh;
-            qf[c] = live && e < g.P ? frag_load<T>(qp + e) : frag_zero<T>();
+            qf[c] = hi > 0 && e < g.P ? frag_load<T>(qp + e) : frag_zero<T>();
         }
     }
 
@@ -325,7 +346,8 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
     // first of a wave the smallest
     const int jlast = min(min(r0 + BM, rows) - 1, sq.q_len * g.pack - 1) / g.pack;
     const int hi_all = r0 < sq.q_len * g.pack ? sq.hi(g, jlast) : 0;
-    const int wrow = r0 + 32 * wq, hi_low = wrow + 31 < sq.q_len * g.pack ? sq.hi(g, wrow / g.pack) : 0;
+    // (rows without a query need no mask: their sums are dropped at the end)
+    const int wrow = r0 + 32 * wq, hi_low = wrow < sq.q_len * g.pack ? sq.hi(g, wrow / g.pack) : INT32_MAX;
     int2 qr{0, 0};
     int onedoc = -1;  // the document of all the wave's rows, if one
     if (g.doc) {
@@ -342,20 +364,28 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
     const int s_end = min(steps, (split + 1) * per);
     int s = split * per;
     const int nr = (g.K + STREAM_RANGE - 1) / STREAM_RANGE;
-    // next step from s on whose keys may be of the rows' documents
+    Window win{-64, 0, 0, 0};
+    auto read = [&](int from) {
+        int4 r[BN / STREAM_RANGE];
+        bool meet = false, holes = false, whole = onedoc >= 0;
+#pragma unroll
+        for (int i = 0; i < BN / STREAM_RANGE; ++i) {
+            const int e = (from + lane) * (BN / STREAM_RANGE) + i;
+            r[i] = e < nr ? g.ranges[(int64_t)b * nr + e] : int4{INT32_MAX, -1, 1, 0};
+            meet = meet || ranges_meet(r[i], qr);
+            holes = holes || r[i].z != 0;
+            whole = whole && range_is(r[i], onedoc);
+        }
+        win = Window{from, __ballot(meet && from + lane < s_end), __ballot(holes), __ballot(whole)};
+    };
+    // next step from `from` on whose keys may be of the rows' documents
     auto next = [&](int from) {
         if (!g.doc) return from;
-        for (; from < s_end; from += 64) {
-            bool in = false;
-            if (from + lane < s_end) {
-#pragma unroll
-                for (int i = 0; i < BN / STREAM_RANGE; ++i) {
-                    const int e = (from + lane) * (BN / STREAM_RANGE) + i;
-                    if (e < nr) in |= ranges_meet(g.ranges[(int64_t)b * nr + e], qr);
-                }
-            }
-            const uint64_t m = __ballot(in);
+        while (from < s_end) {
+            if (from >= win.base + 64) read(from);
+            const uint64_t m = win.meet >> (from - win.base);
             if (m) return from + (int)__builtin_ctzll(m);
+            from = win.base + 64;
         }
         return s_end;
     };
@@ -367,17 +397,6 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
     ck.init(tid, g.P, g.k.st);
     cv.init(tid, g.P, g.v.st);
     const uint32_t base = lds_offset(lds);
-    // keys of a step without a hole, and of one document
-    auto whole = [&](int step, int id) {
-        bool w = true;
-#pragma unroll
-        for (int i = 0; i < BN / STREAM_RANGE; ++i) {
-            const int e = step * (BN / STREAM_RANGE) + i;
-            const int4 r = e < nr ? g.ranges[(int64_t)b * nr + e] : int4{0, 0, 1, 0};
-            w = w && (id < 0 ? r.z == 0 : range_is(r, id));
-        }
-        return w;
-    };
     int fdoc = -1;  // documents of the step on its way, in LDS once its turn is near (put)
     auto put = [&](int buf) {
         if (docs && tid < BN) kdoc[buf * BN + tid] = fdoc;
@@ -385,7 +404,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
     auto fetch = [&](int step, int buf) {
         const int k0 = step * BN;
         if (docs && tid < BN) fdoc = k0 + tid < sq.k_len ? docs[k0 + tid] : -1;
-        const bool all = !docs || whole(step, -1);
+        const bool all = !docs || !win.is(win.holes, step);
         auto in = [&](int r) { return k0 + r < sq.k_len && docs[k0 + r] >= 0; };
         const uint32_t to = base + (uint32_t)(buf * 2 * TB);
         ck.issue(tid, reinterpret_cast<const char*>(kp + (int64_t)k0 * g.k.st), sq.k_len - k0, to, all, in);
@@ -397,9 +416,9 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
     for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-    // m: in units of the products (or of what the bias made of them)
+    // m: in the scores' own units
     float m = -INFINITY, l = 0.f;
-    const float f = sc.factor(), slack = 8.f / f;
+    const float f = BIAS ? 1.f : sc.scale, slack = 8.f / f;
 
     s = next(s);
     if (s < s_end) {
@@ -409,35 +428,32 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
     for (int buf = 0; s < s_end; buf ^= NB - 1) {
         copied();
         __syncthreads();
-        const int step = s, k0 = s * BN + 32 * NS * wk;  // this wave's keys
+        const int k0 = s * BN + 32 * NS * wk;  // this wave's keys
+        const bool mixed = docs && !win.is(win.whole, s);
         const char *tk = lds + buf * 2 * TB, *tv = tk + TB;
         s = next(s + 1);
         if (NB == 2 && s < s_end) fetch(s, buf ^ 1);
 
-        floatx16 x[NS];
+        floatx16 a[NS];
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[n][i] = 0.f;
+            for (int i = 0; i < 16; ++i) a[n][i] = 0.f;
 #pragma unroll
             for (int c = 0; c < NC; ++c)
-                x[n] = mma<T>(TL::row(tk, 32 * (NS * wk + n) + c32, 16 * c + 8 * hh), qf[c], x[n]);
+                a[n] = mma<T>(TL::row(tk, 32 * (NS * wk + n) + c32, 16 * c + 8 * hh), qf[c], a[n]);
         }
-        if constexpr (CAP) {
+        float x[NS][16];
+        const float far = BIAS ? (float)(pos - k0 - 4 * hh) : 0.f;
 #pragma unroll
-            for (int n = 0; n < NS; ++n)
+        for (int n = 0; n < NS; ++n)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[n][i] = cap_tanh<T>(x[n][i] * sc.rcap);
-        }
-        if (sc.bias) {
-            const float far = (float)(pos - k0 - 4 * hh);
-#pragma unroll
-            for (int n = 0; n < NS; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
+            for (int i = 0; i < 16; ++i) {
+                x[n][i] = sc.value(a[n][i]);
+                if constexpr (BIAS)
                     x[n][i] = fmaf(-slope2, fabsf(far - (float)(32 * n + 8 * (i >> 2) + (i & 3))), x[n][i] * sc.scale);
-        }
-        if (docs && !(onedoc >= 0 && whole(step, onedoc))) {
+            }
+        if (mixed) {
 #pragma unroll
             for (int n = 0; n < NS; ++n)
 #pragma unroll
@@ -446,7 +462,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
                     const int id[4] = {kd.x, kd.y, kd.z, kd.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (id[i] != mydoc || mydoc < 0) x[n][4 * q + i] = -INFINITY;
+                        if (id[i] != mydoc) x[n][4 * q + i] = -INFINITY;
                 }
         }
         if (k0 + 32 * NS > hi_low) {
@@ -501,7 +517,11 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
             put(0);
         }
     }
-    m *= f;  // from here in units of log2
+    m = m * f + sc.offset;  // from here in units of log2
+    if (hi == 0) {  // a row that sees nothing
+        m = -INFINITY;
+        l = 0.f;
+    }
     l += other_half(l);
 
     if constexpr (WK > 1) {
@@ -611,40 +631,44 @@ __global__ __launch_bounds__(NT) void join_k(StreamArgs g) {
 
 // ------------------------------------------------------------ backward
 // Row terms D = dout . out, out as the forward had it before rounding (its
-// stored value and the saved rest): 16 lanes a row, 16 rows a step of a
-// block.  fp16 also: the largest |dout| of every 256 rows of a head, from
-// which the score gradients get a power of two that keeps them out of the
-// type's subnormal numbers (a probability of 1e-5 times a small gradient
-// would lose its bits there).
-template <typename T>
+// stored value and the saved rest): LPR lanes a row, 8 elements each, four
+// rows of a lane group requested together.  fp16 also: the largest |dout| of
+// every 256 rows of a head, from which the score gradients get a power of
+// two that keeps them out of the type's subnormal numbers (a probability of
+// 1e-5 times a small gradient would lose its bits there).
+template <typename T, int LPR>
 __global__ __launch_bounds__(NT) void rows_k(StreamArgs g) {
+    constexpr int RPB = NT / LPR, U = 4;
     const int nch = (g.J + STREAM_DROWS - 1) / STREAM_DROWS, z = (int)blockIdx.x / nch, ch = (int)blockIdx.x - z * nch;
-    const int b = z / g.H, h = z - b * g.H, gl = threadIdx.x & 15;
+    const int b = z / g.H, h = z - b * g.H, gl = threadIdx.x % LPR, e = min(8 * gl, g.P - 8);
     const Seq s(g, b);
+    const T* dp = reinterpret_cast<const T*>(g.dout.ptr) + b * g.dout.sb + h * g.dout.sh + e;
+    const T* op = reinterpret_cast<const T*>(g.o.ptr) + b * g.o.sb + h * g.o.sh + e;
+    const T* lp = reinterpret_cast<const T*>(g.lo) + ((int64_t)b * g.J * g.H + h) * g.P + e;
     float top = 0.f;
-    for (int r = threadIdx.x >> 4; r < STREAM_DROWS; r += NT / 16) {
-        const int j = ch * STREAM_DROWS + r;
-        if (j >= g.J) break;
-        float d = 0.f;
-        const bool in = j < s.q_len && !(g.doc && s.doc_of(g, b, j) < 0);
-        if (in && 8 * gl < g.P) {
-            float a[8], y[8];
-            V8<T>::load(reinterpret_cast<const T*>(g.dout.ptr) + b * g.dout.sb + h * g.dout.sh + j * g.dout.st + 8 * gl, a);
-            V8<T>::load(reinterpret_cast<const T*>(g.o.ptr) + b * g.o.sb + h * g.o.sh + j * g.o.st + 8 * gl, y);
-            if constexpr (sizeof(T) == 2) {
-                float lo[8];
-                V8<T>::load(reinterpret_cast<const T*>(g.lo) + (((int64_t)b * g.J + j) * g.H + h) * g.P + 8 * gl, lo);
+    for (int r0 = 0; r0 < STREAM_DROWS; r0 += RPB * U) {
+        float a[U][8], y[U][8], lo[U][8];
+        bool in[U];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] += lo[i];
-            }
+        for (int u = 0; u < U; ++u) {
+            const int row = ch * STREAM_DROWS + r0 + u * RPB + threadIdx.x / LPR, j = min(row, g.J - 1);
+            in[u] = row < s.q_len && 8 * gl < g.P && !(g.doc && s.doc_of(g, b, j) < 0);
+            V8<T>::load(dp + (int64_t)j * g.dout.st, a[u]);
+            V8<T>::load(op + (int64_t)j * g.o.st, y[u]);
+            if constexpr (sizeof(T) == 2) V8<T>::load(lp + (int64_t)j * g.H * g.P, lo[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int row = ch * STREAM_DROWS + r0 + u * RPB + threadIdx.x / LPR;
+            float d = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                d = fmaf(a[i], y[i], d);
-                top = fmaxf(top, fabsf(a[i]));
+                d = fmaf(a[u][i], sizeof(T) == 2 ? y[u][i] + lo[u][i] : y[u][i], d);
+                if (in[u]) top = fmaxf(top, fabsf(a[u][i]));
             }
+            d = group_sum<LPR>(in[u] ? d : 0.f);
+            if (gl == 0 && row < g.J) g.dsum[(int64_t)z * g.J + row] = d;
         }
-        d = group_sum<16>(d);
-        if (gl == 0) g.dsum[(int64_t)z * g.J + j] = d;
     }
     if (g.dmax) {
         __shared__ float w[NT / 64];
@@ -690,7 +714,7 @@ template <typename T> __device__ __forceinline__ void hold_overflow(bool on) {
 // dK and dV of 128 keys (32 a wave) of one key/value head: walks the query
 // rows of its query heads (of a part of them where the heads are split),
 // 64 a step.
-template <typename T, int DP, bool CAP>
+template <typename T, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k(StreamArgs g) {
     constexpr int BQ = 64, ND = DP / 32, NC = DP / 16;
     using TL = Tile<T, DP>;
@@ -711,7 +735,7 @@ __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k(
     const int key = k0 + 32 * wave + c32;
     const int kd = docs ? (key < sq.k_len ? docs[key] : -1) : 0;
     const bool kin = key < sq.k_len && kd >= 0;
-    const Scorer sc(g);
+    const Scorer<T, CAP, BIAS> sc(g);
     const Gain gn = gain<T>(g, b, kvh);
 
     Frag<T> kf[NC], vf[NC];
@@ -755,13 +779,19 @@ __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k(
         const int p = sq.off + step * BQ + i * (BQ - 1), e = max(p, 0) / STREAM_RANGE;
         return p >= 0 && e < nr ? g.ranges[(int64_t)b * nr + e] : int4{INT32_MAX, -1, 1, 0};
     };
+    Window win{-64, 0, 0, 0};
     auto next = [&](int from) {
         if (!docs) return from;
-        for (; from < nst; from += 64) {
-            const bool in = from + lane < nst &&
-                            (ranges_meet(entry(from + lane, 0), kr) || ranges_meet(entry(from + lane, 1), kr));
-            const uint64_t mk = __ballot(in);
-            if (mk) return from + (int)__builtin_ctzll(mk);
+        while (from < nst) {
+            if (from < win.base || from >= win.base + 64) {
+                const int4 r0 = entry(from + lane, 0), r1 = entry(from + lane, 1);
+                win = Window{from, __ballot(from + lane < nst && (ranges_meet(r0, kr) || ranges_meet(r1, kr))),
+                             __ballot(r0.z != 0 || r1.z != 0),
+                             __ballot(onedoc >= 0 && range_is(r0, onedoc) && range_is(r1, onedoc))};
+            }
+            const uint64_t m = win.meet >> (from - win.base);
+            if (m) return from + (int)__builtin_ctzll(m);
+            from = win.base + 64;
         }
         return nst;
     };
@@ -784,7 +814,7 @@ __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k(
         auto put = [&](int buf) {
             if (tid < BQ) {
                 float* r = rows_of(buf) + tid;
-                r[0] = f_lse;
+                r[0] = f_lse;  // less lse, in the score's units without its offset
                 r[BQ] = f_d;
                 reinterpret_cast<int*>(r)[2 * BQ] = f_hi;
                 reinterpret_cast<int*>(r)[3 * BQ] = f_doc;
@@ -792,12 +822,12 @@ __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k(
         };
         auto fetch = [&](int step, int buf) {
             const int j0 = step * BQ;
-            const bool all = !docs || (entry(step, 0).z == 0 && entry(step, 1).z == 0);
+            const bool all = !docs || !win.is(win.holes, step);
             auto in = [&](int r) { return sq.doc_of(g, b, j0 + r) >= 0; };
             if (tid < BQ) {
                 const int j = j0 + tid;
                 const bool row = j < sq.q_len;
-                f_lse = row ? gn.p2 - g.lse[zr + j] : -INFINITY;
+                f_lse = row ? gn.p2 + sc.offset - g.lse[zr + j] : -INFINITY;
                 f_d = row ? -g.dsum[zr + j] : 0.f;
                 f_hi = sq.hi(g, j);
                 f_doc = docs ? sq.doc_of(g, b, j) : 0;
@@ -815,15 +845,13 @@ __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k(
         for (int buf = 0; s < nst; buf ^= NB - 1) {
             copied();
             __syncthreads();
-            const int step = s, j0 = s * BQ;
+            const int j0 = s * BQ;
+            // (rows behind the last query have zeros and no probabilities)
+            const bool some = k0 + 32 * wave + 32 > sq.hi(g, j0) || (docs && !win.is(win.whole, s));
             const char *tq = lds + buf * STEP, *td = tq + TB;
             const float* rows = rows_of(buf);
             s = next(s + 1);
             if (NB == 2 && s < nst) fetch(s, buf ^ 1);
-            // (rows behind the last query have zeros and no probabilities)
-            const bool bound = k0 + 32 * wave + 32 > sq.hi(g, j0);
-            const bool other = docs && !(onedoc >= 0 && range_is(entry(step, 0), onedoc) &&
-                                         range_is(entry(step, 1), onedoc));
 #pragma unroll
             for (int n = 0; n < BQ / 32; ++n) {
                 floatx16 x, dpd;
@@ -845,25 +873,16 @@ __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k(
                     dpd = mma<T>(TL::row(td, 32 * n + c32, 16 * c + 8 * hh), vf[c], dpd);
                 }
                 float p[16], ds[16];
-                if constexpr (CAP) {
+                const float far = BIAS ? (float)(sq.off + j0 + 32 * n + 4 * hh - key) : 0.f;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        x[i] = cap_tanh<T>(x[i] * sc.rcap);
-                        dpd[i] *= 1.f - x[i] * x[i];
-                    }
+                for (int i = 0; i < 16; ++i) {
+                    const float v = sc.value(x[i]);
+                    float e = fmaf(v, sc.scale, nl[i]);
+                    if constexpr (BIAS) e = fmaf(-slope2, fabsf(far + (float)(8 * (i >> 2) + (i & 3))), e);
+                    p[i] = __builtin_amdgcn_exp2f(e);
+                    ds[i] = CAP ? dpd[i] * sc.slope(v) : dpd[i];
                 }
-                if (sc.bias) {
-                    const float far = (float)(sq.off + j0 + 32 * n + 4 * hh - key);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        p[i] = fmaf(-slope2, fabsf(far + (float)(8 * (i >> 2) + (i & 3))), fmaf(x[i], sc.scale, nl[i]));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) p[i] = fmaf(x[i], sc.scale, nl[i]);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]);
-                if (bound || other) {
+                if (some) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const int* r = reinterpret_cast<const int*>(rows) + 2 * BQ + 32 * n + 8 * q + 4 * hh;
@@ -876,7 +895,7 @@ __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k(
                     }
                 }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) ds[i] = score_grad<T>(p[i], dpd[i], gn);
+                for (int i = 0; i < 16; ++i) ds[i] = score_grad<T>(p[i], ds[i], gn);
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const Frag<T> pf = frag_acc<T>(p + 8 * c), sf = frag_acc<T>(ds + 8 * c);
@@ -898,7 +917,7 @@ __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k(
     }
     if (key >= g.K) return;
     hold_overflow<T>(false);
-    const float fk = g.scaler * gn.dsinv;
+    const float fk = g.scaler * sc.SLOPE * gn.dsinv;
     T* dkp = reinterpret_cast<T*>(g.dk.ptr) + b * g.dk.sb + kvh * g.dk.sh + (int64_t)key * g.dk.st;
     T* dvp = reinterpret_cast<T*>(g.dv.ptr) + b * g.dv.sb + kvh * g.dv.sh + (int64_t)key * g.dv.st;
     float* pk = g.part_k + ((((int64_t)part * g.B + b) * g.G + kvh) * g.K + key) * 2 * g.P;
@@ -945,7 +964,7 @@ __global__ __launch_bounds__(NT) void dkv_join_k(StreamArgs g) {
 
 // dQ of 128 query rows (32 a wave) of one head: walks their keys as the
 // forward does.
-template <typename T, int DP, bool CAP>
+template <typename T, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NT, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void dq_k(StreamArgs g) {
     constexpr int BM = 128, BN = 64, NS = 2, ND = DP / 32, NC = DP / 16;
     using TL = Tile<T, DP>;
@@ -967,10 +986,10 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void dq_k(S
     const bool live = j < sq.q_len && mydoc >= 0;
     const int hi = live ? sq.hi(g, j) : 0;
     const float slope2 = g.slopes ? g.slopes[h] * LOG2E : 0.f;
-    const Scorer sc(g);
+    const Scorer<T, CAP, BIAS> sc(g);
     const Gain gn = gain<T>(g, b, kvh);
     const int64_t zr = ((int64_t)b * g.H + h) * g.J + j;
-    const float nl = live ? gn.p2 - g.lse[zr] : -INFINITY, nd = live ? -g.dsum[zr] : 0.f;
+    const float nl = live ? gn.p2 + sc.offset - g.lse[zr] : -INFINITY, nd = live ? -g.dsum[zr] : 0.f;
 
     Frag<T> qf[NC], df[NC];
     {
@@ -979,13 +998,14 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void dq_k(S
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int e = 16 * c + 8 * hh;
-            qf[c] = live && e < g.P ? frag_load<T>(qp + e) : frag_zero<T>();
+            qf[c] = hi > 0 && e < g.P ? frag_load<T>(qp + e) : frag_zero<T>();
             df[c] = live && e < g.P ? frag_load<T>(dp + e) : frag_zero<T>();
         }
     }
     const int jlast = min(min(j0 + BM, g.J), sq.q_len) - 1, wj = j0 + 32 * wave;
     const int steps = j0 < sq.q_len ? (sq.hi(g, jlast) + BN - 1) / BN : 0;
-    const int hi_low = wj + 31 < sq.q_len ? sq.hi(g, wj) : 0;
+    // (rows without a query have no probabilities)
+    const int hi_low = wj < sq.q_len ? sq.hi(g, wj) : INT32_MAX;
     int2 qr{0, 0};
     int onedoc = -1;
     if (docs) {
@@ -999,12 +1019,18 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void dq_k(S
     }
     const int nr = (g.K + STREAM_RANGE - 1) / STREAM_RANGE;
     const int4* ranges = g.ranges + (int64_t)b * nr;
+    Window win{-64, 0, 0, 0};
     auto next = [&](int from) {
         if (!docs) return from;
-        for (; from < steps; from += 64) {
-            const bool in = from + lane < steps && ranges_meet(ranges[from + lane], qr);
-            const uint64_t mk = __ballot(in);
-            if (mk) return from + (int)__builtin_ctzll(mk);
+        while (from < steps) {
+            if (from >= win.base + 64) {
+                const int4 r = from + lane < steps ? ranges[from + lane] : int4{INT32_MAX, -1, 1, 0};
+                win = Window{from, __ballot(ranges_meet(r, qr)), __ballot(r.z != 0),
+                             __ballot(onedoc >= 0 && range_is(r, onedoc))};
+            }
+            const uint64_t m = win.meet >> (from - win.base);
+            if (m) return from + (int)__builtin_ctzll(m);
+            from = win.base + 64;
         }
         return steps;
     };
@@ -1021,7 +1047,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void dq_k(S
     auto fetch = [&](int step, int buf) {
         const int k0 = step * BN;
         if (docs && tid < BN) fdoc = k0 + tid < sq.k_len ? docs[k0 + tid] : -1;
-        const bool all = !docs || ranges[step].z == 0;
+        const bool all = !docs || !win.is(win.holes, step);
         auto in = [&](int r) { return k0 + r < sq.k_len && docs[k0 + r] >= 0; };
         const uint32_t to = base + (uint32_t)(buf * 2 * TB);
         ck.issue(tid, reinterpret_cast<const char*>(kp + (int64_t)k0 * g.k.st), sq.k_len - k0, to, all, in);
@@ -1044,7 +1070,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void dq_k(S
         __syncthreads();
         const int k0 = s * BN;
         const char *tk = lds + buf * 2 * TB, *tv = tk + TB;
-        const bool other = docs && !(onedoc >= 0 && range_is(ranges[s], onedoc));
+        const bool mixed = docs && !win.is(win.whole, s);
         s = next(s + 1);
         if (NB == 2 && s < steps) fetch(s, buf ^ 1);
 #pragma unroll
@@ -1061,25 +1087,16 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void dq_k(S
                 dpd = mma<T>(TL::row(tv, 32 * n + c32, 16 * c + 8 * hh), df[c], dpd);
             }
             float p[16], ds[16];
-            if constexpr (CAP) {
+            const float far = BIAS ? (float)(pos - k0 - 32 * n - 4 * hh) : 0.f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    x[i] = cap_tanh<T>(x[i] * sc.rcap);
-                    dpd[i] *= 1.f - x[i] * x[i];
-                }
+            for (int i = 0; i < 16; ++i) {
+                const float v = sc.value(x[i]);
+                float e = fmaf(v, sc.scale, nl);
+                if constexpr (BIAS) e = fmaf(-slope2, fabsf(far - (float)(8 * (i >> 2) + (i & 3))), e);
+                p[i] = __builtin_amdgcn_exp2f(e);
+                ds[i] = CAP ? dpd[i] * sc.slope(v) : dpd[i];
             }
-            if (sc.bias) {
-                const float far = (float)(pos - k0 - 32 * n - 4 * hh);
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    p[i] = fmaf(-slope2, fabsf(far - (float)(8 * (i >> 2) + (i & 3))), fmaf(x[i], sc.scale, nl));
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) p[i] = fmaf(x[i], sc.scale, nl);
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]);
-            if (other) {
+            if (mixed) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int4 kd = *reinterpret_cast<const int4*>(kdoc + buf * BN + 32 * n + 8 * q + 4 * hh);
@@ -1096,7 +1113,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void dq_k(S
                     if (8 * (i >> 2) + (i & 3) >= end) p[i] = 0.f;
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) ds[i] = score_grad<T>(p[i], dpd[i], gn);
+            for (int i = 0; i < 16; ++i) ds[i] = score_grad<T>(p[i], ds[i], gn);
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const Frag<T> sf = frag_acc<T>(ds + 8 * c);
@@ -1115,7 +1132,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void dq_k(S
     if (j >= g.J) return;
     hold_overflow<T>(false);
     T* dqp = reinterpret_cast<T*>(g.dq.ptr) + b * g.dq.sb + h * g.dq.sh + (int64_t)j * g.dq.st;
-    const float f = g.scaler * gn.dsinv;
+    const float f = g.scaler * sc.SLOPE * gn.dsinv;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -1130,40 +1147,42 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void dq_k(S
 }
 
 // ------------------------------------------------------------- launches
-template <typename T, int DP, bool CAP> void launch_fwd(const StreamArgs& a, bool few, hipStream_t st) {
+template <typename T, int DP, bool CAP, bool BIAS> void launch_fwd(const StreamArgs& a, bool few, hipStream_t st) {
     const int64_t rows = (int64_t)a.J * a.pack, nz = (int64_t)a.B * (a.H / a.pack) * a.splits;
     if (few)
-        fwd_k<T, DP, CAP, 1, 1><<<dim3((unsigned)((rows + 31) / 32 * nz)), NT, 0, st>>>(a);
+        fwd_k<T, DP, CAP, BIAS, 1, 1><<<dim3((unsigned)((rows + 31) / 32 * nz)), NT, 0, st>>>(a);
     else
-        fwd_k<T, DP, CAP, 4, 2><<<dim3((unsigned)((rows + STREAM_BM - 1) / STREAM_BM * nz)), NT, 0, st>>>(a);
+        fwd_k<T, DP, CAP, BIAS, 4, 2><<<dim3((unsigned)((rows + STREAM_BM - 1) / STREAM_BM * nz)), NT, 0, st>>>(a);
 }
 
-template <typename T, int DP, bool CAP> void launch_bwd(const StreamArgs& a, hipStream_t st) {
+template <typename T, int DP, bool CAP, bool BIAS> void launch_bwd(const StreamArgs& a, hipStream_t st) {
     const int64_t nk = (int64_t)((a.K + STREAM_KEYS - 1) / STREAM_KEYS) * a.B * a.G;
     const int64_t nq = (int64_t)((a.J + 127) / 128) * a.B * a.H;
-    if (nk > 0) dkv_k<T, DP, CAP><<<dim3((unsigned)(nk * a.hparts)), NT, 0, st>>>(a);
+    if (nk > 0) dkv_k<T, DP, CAP, BIAS><<<dim3((unsigned)(nk * a.hparts)), NT, 0, st>>>(a);
     if (nk > 0 && a.hparts > 1) {
         const int64_t n = (int64_t)a.B * a.G * a.K * (2 * a.P / 8);
         dkv_join_k<T><<<dim3((unsigned)((n + NT - 1) / NT)), NT, 0, st>>>(a);
     }
-    if (nq > 0) dq_k<T, DP, CAP><<<dim3((unsigned)nq), NT, 0, st>>>(a);
+    if (nq > 0) dq_k<T, DP, CAP, BIAS><<<dim3((unsigned)nq), NT, 0, st>>>(a);
+}
+
+// fn(head size, capped, biased) as compile-time values
+template <typename Fn> void pick(const StreamArgs& a, Fn fn) {
+    auto bias = [&](auto dp, auto cap) {
+        if (a.slopes) fn(dp, cap, std::true_type{});
+        else fn(dp, cap, std::false_type{});
+    };
+    auto cap = [&](auto dp) {
+        if (a.cap > 0.f) bias(dp, std::true_type{});
+        else bias(dp, std::false_type{});
+    };
+    const int dp = stream_head_pad(a.P);
+    if (dp == 32) cap(std::integral_constant<int, 32>{});
+    else if (dp == 64) cap(std::integral_constant<int, 64>{});
+    else cap(std::integral_constant<int, 128>{});
 }
 
 }  // namespace stream
-
-#define DM_STREAM_PICK(FN, ...)                                         \
-    do {                                                                \
-        const int dp_ = stream_head_pad(a.P);                           \
-        if (a.cap > 0.f) {                                              \
-            if (dp_ == 32) stream::FN<T, 32, true>(__VA_ARGS__);        \
-            else if (dp_ == 64) stream::FN<T, 64, true>(__VA_ARGS__);   \
-            else stream::FN<T, 128, true>(__VA_ARGS__);                 \
-        } else {                                                        \
-            if (dp_ == 32) stream::FN<T, 32, false>(__VA_ARGS__);       \
-            else if (dp_ == 64) stream::FN<T, 64, false>(__VA_ARGS__);  \
-            else stream::FN<T, 128, false>(__VA_ARGS__);                \
-        }                                                               \
-    } while (0)
 
 // (a launch without blocks is an error: what has no rows or keys is left out)
 inline int64_t stream_ranges_n(const StreamArgs& a) {
@@ -1172,7 +1191,9 @@ inline int64_t stream_ranges_n(const StreamArgs& a) {
 
 template <typename T> void stream_fwd(const StreamArgs& a, bool few, hipStream_t st) {
     if (a.doc && a.K > 0) stream::ranges_k<T><<<dim3((unsigned)stream_ranges_n(a)), 64, 0, st>>>(a);
-    DM_STREAM_PICK(launch_fwd, a, few, st);
+    stream::pick(a, [&](auto dp, auto cap, auto bias) {
+        stream::launch_fwd<T, decltype(dp)::value, decltype(cap)::value, decltype(bias)::value>(a, few, st);
+    });
     if (a.splits > 1) {
         const int64_t lanes = (int64_t)a.B * a.H * a.J * 16;
         stream::join_k<T><<<dim3((unsigned)((lanes + stream::NT - 1) / stream::NT)), stream::NT, 0, st>>>(a);
@@ -1183,9 +1204,13 @@ template <typename T> void stream_bwd(const StreamArgs& a, hipStream_t st) {
     if (a.doc && a.K > 0) stream::ranges_k<T><<<dim3((unsigned)stream_ranges_n(a)), 64, 0, st>>>(a);
     if (a.J > 0) {
         const int64_t n = (int64_t)((a.J + STREAM_DROWS - 1) / STREAM_DROWS) * a.B * a.H;
-        stream::rows_k<T><<<dim3((unsigned)n), stream::NT, 0, st>>>(a);
+        if (a.P <= 32) stream::rows_k<T, 4><<<dim3((unsigned)n), stream::NT, 0, st>>>(a);
+        else if (a.P <= 64) stream::rows_k<T, 8><<<dim3((unsigned)n), stream::NT, 0, st>>>(a);
+        else stream::rows_k<T, 16><<<dim3((unsigned)n), stream::NT, 0, st>>>(a);
     }
-    DM_STREAM_PICK(launch_bwd, a, st);
+    stream::pick(a, [&](auto dp, auto cap, auto bias) {
+        stream::launch_bwd<T, decltype(dp)::value, decltype(cap)::value, decltype(bias)::value>(a, st);
+    });
 }
 
 }  // namespace dm
