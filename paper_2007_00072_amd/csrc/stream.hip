@@ -27,8 +27,8 @@ int key_splits(const dm_attn_desc& d) {
     const int64_t pack = packed_heads(d);
     const int64_t blocks = ((int64_t)d.J * pack + bm - 1) / bm * d.B * (d.H / pack);
     const int64_t steps = (d.K + bn - 1) / bn, least = few ? 2 : 4;
-    if (blocks == 0 || blocks >= 384) return 1;
-    int64_t s = (512 + blocks - 1) / blocks;
+    if (blocks == 0 || blocks >= (few ? 1024 : 384)) return 1;
+    int64_t s = ((few ? 1024 : 512) + blocks - 1) / blocks;
     if (s > steps / least) s = steps / least;
     return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
 }

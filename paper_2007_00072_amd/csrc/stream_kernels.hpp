@@ -150,21 +150,25 @@ __device__ __forceinline__ void copy16(uint32_t lds, uint32_t voff, u32x4 rsrc) 
                  : "memory");
 }
 __device__ __forceinline__ void copied() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// all copies but the last N of this wave
+template <int N> __device__ __forceinline__ void copied_but() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// this wave's LDS reads so far
+__device__ __forceinline__ void lds_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 
-template <typename T, int DP, int ROWS> struct Copies {
+template <typename T, int DP, int ROWS, int LANES = NT> struct Copies {
     using TL = Tile<T, DP>;
-    static constexpr int N = ROWS * TL::PIECES / NT;
-    static_assert(ROWS * TL::PIECES % NT == 0, "pieces");
+    static constexpr int N = ROWS * TL::PIECES / LANES;
+    static_assert(ROWS * TL::PIECES % LANES == 0, "pieces");
     static constexpr uint32_t NONE = 0xfffffff0u;  // behind any end
     uint32_t vo[N];
     uint32_t step;  // bytes between rows
-    __device__ __forceinline__ int row(int tid, int i) const { return (i * NT + tid) / TL::PIECES; }
+    __device__ __forceinline__ int row(int tid, int i) const { return (i * LANES + tid) / TL::PIECES; }
     __device__ __forceinline__ void init(int tid, int P, int64_t st) {
         step = (uint32_t)(st * (int64_t)sizeof(T));
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int r = row(tid, i), c = (i * NT + tid) % TL::PIECES ^ swz<TL::PITCH>(r);
+            const int r = row(tid, i), c = (i * LANES + tid) % TL::PIECES ^ swz<TL::PITCH>(r);
             vo[i] = c * TL::EPP < P ? (uint32_t)r * step + (uint32_t)c * 16 : NONE;
         }
     }
@@ -179,7 +183,7 @@ template <typename T, int DP, int ROWS> struct Copies {
         for (int i = 0; i < N; ++i) {
             uint32_t v = vo[i];
             if (!all && !in(row(tid, i))) v = NONE;
-            copy16(uniform(to + (uint32_t)i * (NT * 16)), v, rsrc);
+            copy16(uniform(to + (uint32_t)i * (LANES * 16)), v, rsrc);
         }
     }
 };
@@ -299,17 +303,26 @@ __device__ __forceinline__ void place(int nz, int& tile, int& z) {
 // ------------------------------------------------------------- forward
 // A block takes 32 WQ query rows; its waves lie WQ along the queries and
 // WK = 4 / WQ along the keys of a step (each wave 32 NS of them).
+// WQ = 4: the waves share the step's tiles, of which one pair is filled
+// while the other is read.
+// WQ = 1, few rows: reading the keys is what takes time.  Each wave copies
+// its own 32 keys of a step and waits for nobody else; a pair of tiles is
+// asked for as soon as it has been read, so that two steps are on their way
+// whenever the wave waits (with shared tiles, a barrier and one step on its
+// way at a time 165 us where this takes 129: 64 sequences of up to 8192 keys
+// in 4 key/value heads of 128).
 template <typename T, int DP, bool CAP, bool BIAS, int WQ, int NS>
 __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(StreamArgs g) {
     constexpr int WK = 4 / WQ, BM = 32 * WQ, BN = 32 * WK * NS, ND = DP / 32, NC = DP / 16;
+    constexpr bool OWN = WK > 1;  // tiles of a wave's own
     using TL = Tile<T, DP>;
-    constexpr int TB = BN * TL::PITCH;
-    // two steps' tiles where LDS holds them: one is filled while the other is read
+    constexpr int TB = BN * TL::PITCH;  // bytes of a step's keys
     constexpr int NB = 4 * TB <= 131072 ? 2 : 1;
+    constexpr int ROWS = OWN ? 32 * NS : BN, RB = ROWS * TL::PITCH;  // of a tile
     // joining the waves along the keys: m, l and o of all but the first
     constexpr int JOIN = WK > 1 ? (WK - 1) * 64 * (2 + 16 * ND) * 4 : 0;
     constexpr int TILES = 2 * NB * TB > JOIN ? 2 * NB * TB : JOIN;
-    __shared__ __attribute__((aligned(16))) char lds[TILES + 2 * BN * 4];
+    __shared__ __attribute__((aligned(16))) char lds[TILES + (OWN ? 0 : 2 * BN * 4)];
     int* kdoc = reinterpret_cast<int*>(lds + TILES);
 
     const int hz = g.H / g.pack, rows = g.J * g.pack, nqt = (rows + BM - 1) / BM;
@@ -362,7 +375,6 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
     }
     const int steps = (hi_all + BN - 1) / BN, per = (steps + g.splits - 1) / g.splits;
     const int s_end = min(steps, (split + 1) * per);
-    int s = split * per;
     const int nr = (g.K + STREAM_RANGE - 1) / STREAM_RANGE;
     Window win{-64, 0, 0, 0};
     auto read = [&](int from) {
@@ -393,22 +405,24 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
     const T* kp = reinterpret_cast<const T*>(g.k.ptr) + b * g.k.sb + kvh * g.k.sh;
     const T* vp = reinterpret_cast<const T*>(g.v.ptr) + b * g.v.sb + kvh * g.v.sh;
     const int32_t* docs = g.doc ? g.doc + (int64_t)b * g.K : nullptr;
-    Copies<T, DP, BN> ck, cv;
-    ck.init(tid, g.P, g.k.st);
-    cv.init(tid, g.P, g.v.st);
-    const uint32_t base = lds_offset(lds);
+    // (a wave's own tiles lie together: K and V of one step, then of the other)
+    const int who = OWN ? lane : tid, own = OWN ? wave * 2 * NB * RB : 0;
+    Copies<T, DP, ROWS, OWN ? 64 : NT> ck, cv;
+    ck.init(who, g.P, g.k.st);
+    cv.init(who, g.P, g.v.st);
+    const uint32_t base = lds_offset(lds) + (uint32_t)own;
     int fdoc = -1;  // documents of the step on its way, in LDS once its turn is near (put)
     auto put = [&](int buf) {
-        if (docs && tid < BN) kdoc[buf * BN + tid] = fdoc;
+        if (!OWN && docs && tid < BN) kdoc[buf * BN + tid] = fdoc;
     };
     auto fetch = [&](int step, int buf) {
-        const int k0 = step * BN;
-        if (docs && tid < BN) fdoc = k0 + tid < sq.k_len ? docs[k0 + tid] : -1;
+        const int k0 = step * BN + (OWN ? ROWS * wk : 0);
+        if (!OWN && docs && tid < BN) fdoc = k0 + tid < sq.k_len ? docs[k0 + tid] : -1;
         const bool all = !docs || !win.is(win.holes, step);
         auto in = [&](int r) { return k0 + r < sq.k_len && docs[k0 + r] >= 0; };
-        const uint32_t to = base + (uint32_t)(buf * 2 * TB);
-        ck.issue(tid, reinterpret_cast<const char*>(kp + (int64_t)k0 * g.k.st), sq.k_len - k0, to, all, in);
-        cv.issue(tid, reinterpret_cast<const char*>(vp + (int64_t)k0 * g.v.st), sq.k_len - k0, to + TB, all, in);
+        const uint32_t to = base + (uint32_t)(buf * 2 * RB);
+        ck.issue(who, reinterpret_cast<const char*>(kp + (int64_t)k0 * g.k.st), sq.k_len - k0, to, all, in);
+        cv.issue(who, reinterpret_cast<const char*>(vp + (int64_t)k0 * g.v.st), sq.k_len - k0, to + RB, all, in);
     };
 
     floatx16 o[ND];
@@ -420,19 +434,34 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
     float m = -INFINITY, l = 0.f;
     const float f = BIAS ? 1.f : sc.scale, slack = 8.f / f;
 
-    s = next(s);
-    if (s < s_end) {
-        fetch(s, 0);
+    auto mixed = [&](int step) { return docs && step < s_end && !win.is(win.whole, step); };
+    int cur = next(split * per), nxt = s_end;
+    bool cur_mixed = mixed(cur), nxt_mixed = false;
+    if (cur < s_end) {
+        fetch(cur, 0);
         put(0);
+        if (OWN && NB == 2) {
+            nxt = next(cur + 1);
+            nxt_mixed = mixed(nxt);
+            if (nxt < s_end) fetch(nxt, 1);
+        }
     }
-    for (int buf = 0; s < s_end; buf ^= NB - 1) {
-        copied();
-        __syncthreads();
-        const int k0 = s * BN + 32 * NS * wk;  // this wave's keys
-        const bool mixed = docs && !win.is(win.whole, s);
-        const char *tk = lds + buf * 2 * TB, *tv = tk + TB;
-        s = next(s + 1);
-        if (NB == 2 && s < s_end) fetch(s, buf ^ 1);
+    for (int buf = 0; cur < s_end; buf ^= NB - 1) {
+        if (!OWN) {
+            copied();
+            __syncthreads();
+        } else if (NB == 2 && nxt < s_end) {
+            copied_but<2 * Copies<T, DP, ROWS, OWN ? 64 : NT>::N>();
+        } else {
+            copied();
+        }
+        const int k0 = cur * BN + 32 * NS * wk;  // this wave's keys
+        const char *tk = lds + own + buf * 2 * RB, *tv = tk + RB;
+        if (!OWN || NB == 1) {
+            nxt = next(cur + 1);
+            nxt_mixed = mixed(nxt);
+            if (!OWN && NB == 2 && nxt < s_end) fetch(nxt, buf ^ 1);
+        }
 
         floatx16 a[NS];
 #pragma unroll
@@ -441,7 +470,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
             for (int i = 0; i < 16; ++i) a[n][i] = 0.f;
 #pragma unroll
             for (int c = 0; c < NC; ++c)
-                a[n] = mma<T>(TL::row(tk, 32 * (NS * wk + n) + c32, 16 * c + 8 * hh), qf[c], a[n]);
+                a[n] = mma<T>(TL::row(tk, 32 * n + c32, 16 * c + 8 * hh), qf[c], a[n]);
         }
         float x[NS][16];
         const float far = BIAS ? (float)(pos - k0 - 4 * hh) : 0.f;
@@ -453,13 +482,20 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
                 if constexpr (BIAS)
                     x[n][i] = fmaf(-slope2, fabsf(far - (float)(32 * n + 8 * (i >> 2) + (i & 3))), x[n][i] * sc.scale);
             }
-        if (mixed) {
+        if (cur_mixed) {
 #pragma unroll
             for (int n = 0; n < NS; ++n)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int4 kd = *reinterpret_cast<const int4*>(kdoc + buf * BN + 32 * (NS * wk + n) + 8 * q + 4 * hh);
-                    const int id[4] = {kd.x, kd.y, kd.z, kd.w};
+                    const int kk = 32 * n + 8 * q + 4 * hh;
+                    int id[4];
+                    if constexpr (OWN) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) id[i] = docs[min(k0 + kk + i, g.K - 1)];  // (past the end: bounded by hi)
+                    } else {
+                        const int4 kd = *reinterpret_cast<const int4*>(kdoc + buf * BN + kk);
+                        id[0] = kd.x; id[1] = kd.y; id[2] = kd.z; id[3] = kd.w;
+                    }
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (id[i] != mydoc) x[n][4 * q + i] = -INFINITY;
@@ -507,15 +543,28 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
                 const Frag<T> pf = frag_acc<T>(&p[n][8 * c]);
 #pragma unroll
                 for (int d = 0; d < ND; ++d)
-                    o[d] = mma<T>(TL::col(tv, 32 * (NS * wk + n) + 16 * c, 32 * d, lane), pf, o[d]);
+                    o[d] = mma<T>(TL::col(tv, 32 * n + 16 * c, 32 * d, lane), pf, o[d]);
             }
-        if (NB == 2) {
+        int then = nxt;
+        bool then_mixed = nxt_mixed;
+        if (OWN) {
+            lds_read();
+            if (NB == 2 && nxt < s_end) {
+                then = next(nxt + 1);
+                then_mixed = mixed(then);
+            }
+            if (then < s_end && (NB == 1 || then != nxt)) fetch(then, NB == 2 ? buf : 0);
+        } else if (NB == 2) {
             put(buf ^ 1);
         } else {
             __syncthreads();
-            if (s < s_end) fetch(s, 0);
+            if (nxt < s_end) fetch(nxt, 0);
             put(0);
         }
+        cur = nxt;
+        cur_mixed = nxt_mixed;
+        nxt = then;
+        nxt_mixed = then_mixed;
     }
     m = m * f + sc.offset;  // from here in units of log2
     if (hi == 0) {  // a row that sees nothing
