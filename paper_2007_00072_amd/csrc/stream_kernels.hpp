@@ -766,6 +766,7 @@ template <typename T> __device__ __forceinline__ void hold_overflow(bool on) {
 template <typename T, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k(StreamArgs g) {
     constexpr int BQ = 64, ND = DP / 32, NC = DP / 16;
+    constexpr bool FRAGS = sizeof(T) == 2;
     using TL = Tile<T, DP>;
     constexpr int TB = BQ * TL::PITCH;
     // tiles of q and dout, and the rows' numbers: -lse, -D, bounds, documents
@@ -921,6 +922,19 @@ __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k(
                     x = mma<T>(TL::row(tq, 32 * n + c32, 16 * c + 8 * hh), kf[c], x);
                     dpd = mma<T>(TL::row(td, 32 * n + c32, 16 * c + 8 * hh), vf[c], dpd);
                 }
+                // (the second products' fragments are asked for ahead of the
+                // exponentials, which hide the reads)
+                Frag<T> df[2][ND], qf[2][ND];
+                if constexpr (FRAGS) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int d = 0; d < ND; ++d) {
+                            df[c][d] = TL::col(td, 32 * n + 16 * c, 32 * d, lane);
+                            qf[c][d] = TL::col(tq, 32 * n + 16 * c, 32 * d, lane);
+                        }
+                    __builtin_amdgcn_sched_barrier(0x41f);
+                }
                 float p[16], ds[16];
                 const float far = BIAS ? (float)(sq.off + j0 + 32 * n + 4 * hh - key) : 0.f;
 #pragma unroll
@@ -950,8 +964,8 @@ __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k(
                     const Frag<T> pf = frag_acc<T>(p + 8 * c), sf = frag_acc<T>(ds + 8 * c);
 #pragma unroll
                     for (int d = 0; d < ND; ++d) {
-                        dv[d] = mma<T>(TL::col(td, 32 * n + 16 * c, 32 * d, lane), pf, dv[d]);
-                        dk[d] = mma<T>(TL::col(tq, 32 * n + 16 * c, 32 * d, lane), sf, dk[d]);
+                        dv[d] = mma<T>(FRAGS ? df[c][d] : TL::col(td, 32 * n + 16 * c, 32 * d, lane), pf, dv[d]);
+                        dk[d] = mma<T>(FRAGS ? qf[c][d] : TL::col(tq, 32 * n + 16 * c, 32 * d, lane), sf, dk[d]);
                     }
                 }
             }
@@ -1014,7 +1028,7 @@ __global__ __launch_bounds__(NT) void dkv_join_k(StreamArgs g) {
 // dQ of 128 query rows (32 a wave) of one head: walks their keys as the
 // forward does.
 template <typename T, int DP, bool CAP, bool BIAS>
-__global__ __launch_bounds__(NT, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void dq_k(StreamArgs g) {
+__global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void dq_k(StreamArgs g) {
     constexpr int BM = 128, BN = 64, NS = 2, ND = DP / 32, NC = DP / 16;
     using TL = Tile<T, DP>;
     constexpr int TB = BN * TL::PITCH, NB = 4 * TB <= 131072 ? 2 : 1;
@@ -1122,7 +1136,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void dq_k(S
         const bool mixed = docs && !win.is(win.whole, s);
         s = next(s + 1);
         if (NB == 2 && s < steps) fetch(s, buf ^ 1);
-#pragma unroll
+#pragma unroll 1
         for (int n = 0; n < NS; ++n) {
             floatx16 x, dpd;
 #pragma unroll
