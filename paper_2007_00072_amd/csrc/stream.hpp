@@ -39,7 +39,7 @@ constexpr int STREAM_DROWS = 256;  // rows of one entry of `dmax`
 
 // Row tiles and head sizes of the kernels (one function each for the host's
 // grid and the kernels' own constants).
-inline int stream_head_pad(int P) { return P <= 32 ? 32 : P <= 64 ? 64 : 128; }
+inline int stream_head_pad(int P) { return P <= 32 ? 32 : P <= 64 ? 64 : P <= 96 ? 96 : 128; }
 // queries of a block: 4 waves side by side, or all on the same 32 rows, each on keys of its own
 constexpr int STREAM_BM = 128, STREAM_BM_FEW = 32;
 constexpr int STREAM_BN = 64, STREAM_BN_FEW = 128;  // keys of a step

@@ -93,7 +93,7 @@ template <int PITCH> __device__ __forceinline__ int piece_off(int r, int piece) 
 }
 
 template <typename T, int DP> struct Tile {
-    static constexpr int PITCH = DP * (int)sizeof(T);
+    static constexpr int PITCH = (DP == 96 ? 128 : DP) * (int)sizeof(T);
     static constexpr int PIECES = PITCH / 16;       // of a row
     static constexpr int EPP = 16 / (int)sizeof(T);  // elements of a piece
     typedef short s4 __attribute__((ext_vector_type(4)));
@@ -194,8 +194,15 @@ template <typename T> __device__ __forceinline__ void store4(T* p, const float* 
     typedef T T4 __attribute__((ext_vector_type(4)));
     *reinterpret_cast<T4*>(p) = T4{from_f<T>(y[0]), from_f<T>(y[1]), from_f<T>(y[2]), from_f<T>(y[3])};
 }
-// the other lane half's value
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+// both lane halves' values: gfx950 swaps the upper half of one register with
+// the lower half of another (a lane shuffle through the LDS unit would stand
+// in every step's chain of dependent instructions)
+struct Halves { float lo, hi; };
+__device__ __forceinline__ Halves halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    const uint32_t lo = r[0], hi = r[1];
+    return Halves{__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi)};
+}
 
 // Raw products to scores.  With x the returned value, a score in units of
 // log2 is factor x + offset - what the bias takes, and the same for all of a
@@ -514,7 +521,8 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
         for (int n = 0; n < NS; ++n)
 #pragma unroll
             for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, x[n][i]), x[n][i + 1]);
-        mx = fmaxf(mx, other_half(mx));
+        const Halves both = halves(mx);
+        mx = fmaxf(both.lo, both.hi);
         // the row's reference value follows its maximum only once that is 2^8
         // above it: until then sums and products stay far inside their types
         if (__any(mx > m + slack)) {
@@ -571,7 +579,8 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
         m = -INFINITY;
         l = 0.f;
     }
-    l += other_half(l);
+    const Halves sums = halves(l);
+    l = sums.lo + sums.hi;
 
     if constexpr (WK > 1) {
         // join the waves along the keys, in wave order
@@ -1242,6 +1251,7 @@ template <typename Fn> void pick(const StreamArgs& a, Fn fn) {
     const int dp = stream_head_pad(a.P);
     if (dp == 32) cap(std::integral_constant<int, 32>{});
     else if (dp == 64) cap(std::integral_constant<int, 64>{});
+    else if (dp == 96) cap(std::integral_constant<int, 96>{});
     else cap(std::integral_constant<int, 128>{});
 }
 
