@@ -6,7 +6,6 @@ benchmark.
 """
 from __future__ import annotations
 
-import contextlib
 from typing import Dict, Optional, Sequence
 
 import torch
@@ -98,7 +97,7 @@ class MultiHeadAttention:
 
 def _checked(name, t, dtype, shape, device):
     """A tensor's dtype, shape and device as the library will take them for granted."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device:
+    if t.dtype != dtype or t.shape != shape or t.device != device:
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {dtype} {tuple(shape)} on {device}")
     return t
 
@@ -109,11 +108,15 @@ def _dense(name, t, dtype, shape, device):
     return t
 
 
-def _on(device):
-    """The device as the current one during a call, where it is not already."""
-    if device.type != "cuda" or device.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    return torch.cuda.device(device)
+def _launch(device, entry, *args):
+    """An entry point on the device's current stream (and with the device as
+    the current one, where it is not already)."""
+    if device.type != "cuda":
+        return entry(*args)
+    if device.index == torch.cuda.current_device():
+        return entry(*args, stream=torch.cuda.current_stream().cuda_stream)
+    with torch.cuda.device(device):
+        return entry(*args, stream=torch.cuda.current_stream().cuda_stream)
 
 
 def _code(dtype: torch.dtype) -> int:
@@ -163,14 +166,14 @@ class Attention:
 
     def _take(self, name, t):
         """Checks a tensor and puts its strides into the descriptor."""
-        _checked(name, t, self.dtype, self.shapes[name], self.device)
         s = t.stride()
+        if t.dtype != self.dtype or t.shape != self.shapes[name] or t.device != self.device:
+            _checked(name, t, self.dtype, self.shapes[name], self.device)
         if self._strides.get(name) != s:
             if s[3] != 1:
                 raise ValueError(f"{name}: the last axis is not contiguous")
             setattr(self.desc, name, lib.AttnStride(s[0], s[2], s[1]))
             self._strides[name] = s
-        return t
 
     def _like(self, name, t, of):
         """A gradient: shape and strides of its tensor."""
@@ -188,8 +191,7 @@ class Attention:
         if out is None:
             out = torch.empty(self.shapes["out"], dtype=self.dtype, device=self.device)
         self._take("out", out)
-        with _on(self.device):
-            lib.attn_fwd(self.desc, q, k, v, out, self.saved, self.ws, self.ws_bytes)
+        _launch(self.device, lib.attn_fwd, self.desc, q, k, v, out, self.saved, self.ws, self.ws_bytes)
         return out
 
     def backward(self, q, k, v, out, dout, dq=None, dk=None, dv=None):
@@ -202,8 +204,8 @@ class Attention:
         dq = self._empty(q) if dq is None else self._like("dq", dq, q)
         dk = self._empty(k) if dk is None else self._like("dk", dk, k)
         dv = self._empty(v) if dv is None else self._like("dv", dv, v)
-        with _on(self.device):
-            lib.attn_bwd(self.desc, q, k, v, out, self.saved, dout, dq, dk, dv, self.ws, self.ws_bytes)
+        _launch(self.device, lib.attn_bwd, self.desc, q, k, v, out, self.saved, dout, dq, dk, dv, self.ws,
+                self.ws_bytes)
         return dq, dk, dv
 
 
@@ -226,8 +228,7 @@ class Embedding:
         if y is None:
             y = torch.empty((*ids.shape, I), dtype=self.table.dtype, device=self.device)
         _dense("y", y, self.table.dtype, (*ids.shape, I), self.device)
-        with _on(self.device):
-            lib.embed_fwd(self.code, ids.numel(), V, I, ids, self.table, self.scale, y)
+        _launch(self.device, lib.embed_fwd, self.code, ids.numel(), V, I, ids, self.table, self.scale, y)
         return y
 
     def backward(self, ids: torch.Tensor, dy: torch.Tensor) -> torch.Tensor:
@@ -238,9 +239,8 @@ class Embedding:
         need = lib.embed_ws_bytes(ids.numel(), V, I)
         if self.ws.numel() < need:
             self.ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-        with _on(self.device):
-            lib.embed_bwd(self.code, ids.numel(), V, I, ids, self.pad_id, dy, self.scale, self.grad, self.ws,
-                          self.ws.numel())
+        _launch(self.device, lib.embed_bwd, self.code, ids.numel(), V, I, ids, self.pad_id, dy, self.scale,
+                self.grad, self.ws, self.ws.numel())
         return self.grad
 
 
@@ -265,6 +265,7 @@ class AdamW:
         if m is not None:
             state_bits = 32 if m[0].dtype == torch.float32 else 8
         self.params = [_dense("param", p, self.dtype, p.shape, self.device) for p in params]
+        self._shapes = [p.shape for p in params]
         if isinstance(master, str):
             master = [p.float() for p in params] if self.dtype != torch.float32 else None
         sd = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
@@ -302,13 +303,15 @@ class AdamW:
         in place of step, lr and grad_scale."""
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
-        for it, g, p in zip(self._items, grads, self.params):
-            it.grad = _dense("grad", g, torch.float32, p.shape, self.device).data_ptr()
+        f32, dev = torch.float32, self.device
+        for it, g, shape in zip(self._items, grads, self._shapes):
+            if g.dtype != f32 or g.shape != shape or g.device != dev or not g.is_contiguous():
+                _dense("grad", g, f32, shape, dev)
+            it.grad = g.data_ptr()
         if scalars is not None:
             _dense("scalars", scalars, torch.float32, (4,), self.device)
         d = self.desc
         d.step, d.grad_scale, d.scalars = step, grad_scale, lib.ptr(scalars)
         if lr is not None:
             d.lr = lr
-        with _on(self.device):
-            lib.adamw_step(d, self._items, len(self.params))
+        _launch(self.device, lib.adamw_step, d, self._items, len(self.params))
