@@ -43,6 +43,12 @@ inline int stream_head_pad(int P) { return P <= 32 ? 32 : P <= 64 ? 64 : P <= 96
 // queries of a block: 4 waves side by side, or all on the same 32 rows, each on keys of its own
 constexpr int STREAM_BM = 128, STREAM_BM_FEW = 32;
 constexpr int STREAM_BN = 64, STREAM_BN_FEW = 128;  // keys of a step
+// Head sizes above 64: blocks of the backward's two kernels up to which one
+// launch does both.  (There the dK / dV kernel's registers leave one wave a
+// SIMD, with which dQ takes 800 us where its own kernel takes 565, for 8192
+// causal queries in 16 heads of 128; 300 queries in 16 heads take 45 us in
+// one launch and 60 in two.  Up to 64 one launch is never slower.)
+constexpr int STREAM_BOTH = 512;
 constexpr int STREAM_KEYS = 128;                    // keys of a block of the dK / dV kernel
 
 template <typename T> void stream_fwd(const StreamArgs& a, bool few, hipStream_t st);

@@ -295,8 +295,7 @@ struct Window {
 // Block number -> (tile, head): the tiles of a head on one XCD (blocks reach
 // the 8 XCDs in turn), so that its L2 serves the rows they share; all heads'
 // first tiles before the second ones.
-__device__ __forceinline__ void place(int nz, int& tile, int& z) {
-    const int lid = (int)blockIdx.x;
+__device__ __forceinline__ void place(int lid, int nz, int& tile, int& z) {
     if ((nz & 7) == 0) {
         const int hp = nz >> 3, i = lid >> 3;
         tile = i / hp;
@@ -334,7 +333,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
 
     const int hz = g.H / g.pack, rows = g.J * g.pack, nqt = (rows + BM - 1) / BM;
     int tile, z;
-    place(g.B * hz * g.splits, tile, z);
+    place((int)blockIdx.x, g.B * hz * g.splits, tile, z);
     const int split = z % g.splits;
     z /= g.splits;
     if (g.causal) tile = nqt - 1 - tile;  // rows with the most keys first
@@ -772,18 +771,22 @@ template <typename T> __device__ __forceinline__ void hold_overflow(bool on) {
 // dK and dV of 128 keys (32 a wave) of one key/value head: walks the query
 // rows of its query heads (of a part of them where the heads are split),
 // 64 a step.
+template <typename T, int DP> struct DkvTiles {
+    static constexpr int BQ = 64, TB = BQ * Tile<T, DP>::PITCH;
+    // tiles of q and dout, and the rows' numbers: -lse, -D, bounds, documents
+    static constexpr int STEP = 2 * TB + BQ * 16;
+    static constexpr int NB = 2 * STEP <= 131072 + 4096 ? 2 : 1;
+    static constexpr int LDS = NB * STEP;
+};
 template <typename T, int DP, bool CAP, bool BIAS>
-__global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k(StreamArgs g) {
+__device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* lds) {
     constexpr int BQ = 64, ND = DP / 32, NC = DP / 16;
     constexpr bool FRAGS = sizeof(T) == 2;
     using TL = Tile<T, DP>;
-    constexpr int TB = BQ * TL::PITCH;
-    // tiles of q and dout, and the rows' numbers: -lse, -D, bounds, documents
-    constexpr int STEP = 2 * TB + BQ * 16;
-    constexpr int NB = 2 * STEP <= 131072 + 4096 ? 2 : 1;
-    __shared__ __attribute__((aligned(16))) char lds[NB * STEP];
+    using Tiles = DkvTiles<T, DP>;
+    constexpr int TB = Tiles::TB, STEP = Tiles::STEP, NB = Tiles::NB;
     int tile, z;
-    place(g.B * g.G * g.hparts, tile, z);
+    place(block, g.B * g.G * g.hparts, tile, z);
     const int part = z % g.hparts;
     z /= g.hparts;
     const int b = z / g.G, kvh = z - b * g.G, grp = g.H / g.G, k0 = tile * STREAM_KEYS;
@@ -1036,17 +1039,21 @@ __global__ __launch_bounds__(NT) void dkv_join_k(StreamArgs g) {
 
 // dQ of 128 query rows (32 a wave) of one head: walks their keys as the
 // forward does.
+template <typename T, int DP> struct DqTiles {
+    static constexpr int BN = 64, TB = BN * Tile<T, DP>::PITCH, NB = 4 * TB <= 131072 ? 2 : 1;
+    static constexpr int LDS = 2 * NB * TB + 2 * BN * 4 + 4 * 8;  // tiles, documents of the keys, of the waves' rows
+};
 template <typename T, int DP, bool CAP, bool BIAS>
-__global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void dq_k(StreamArgs g) {
+__device__ __forceinline__ void dq_block(const StreamArgs& g, int block, char* lds) {
     constexpr int BM = 128, BN = 64, NS = 2, ND = DP / 32, NC = DP / 16;
     using TL = Tile<T, DP>;
-    constexpr int TB = BN * TL::PITCH, NB = 4 * TB <= 131072 ? 2 : 1;
-    __shared__ __attribute__((aligned(16))) char lds[2 * NB * TB];
-    __shared__ __attribute__((aligned(16))) int kdoc[2 * BN];
-    __shared__ int2 wrange[4];
+    using Tiles = DqTiles<T, DP>;
+    constexpr int TB = Tiles::TB, NB = Tiles::NB;
+    int* kdoc = reinterpret_cast<int*>(lds + 2 * NB * TB);
+    int2* wrange = reinterpret_cast<int2*>(kdoc + 2 * BN);
     const int nqt = (g.J + BM - 1) / BM;
     int tile, z;
-    place(g.B * g.H, tile, z);
+    place(block, g.B * g.H, tile, z);
     if (g.causal) tile = nqt - 1 - tile;
     const int b = z / g.H, h = z - b * g.H, kvh = h / (g.H / g.G);
     const int tid = threadIdx.x, lane = tid & 63, c32 = lane & 31, hh = lane >> 5;
@@ -1218,6 +1225,26 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void dq_k(StreamArgs g)
         }
 }
 
+template <typename T, int DP, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT) void dkv_k(StreamArgs g) {
+    __shared__ __attribute__((aligned(16))) char lds[DkvTiles<T, DP>::LDS];
+    dkv_block<T, DP, CAP, BIAS>(g, (int)blockIdx.x, lds);
+}
+template <typename T, int DP, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void dq_k(StreamArgs g) {
+    __shared__ __attribute__((aligned(16))) char lds[DqTiles<T, DP>::LDS];
+    dq_block<T, DP, CAP, BIAS>(g, (int)blockIdx.x, lds);
+}
+// Both in one launch, so that the end of the one fills with the other:
+// blocks 0 .. nk - 1 (the longer ones) do keys, the others rows.
+template <typename T, int DP, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_dq_k(StreamArgs g, int nk) {
+    constexpr int A = DkvTiles<T, DP>::LDS, B = DqTiles<T, DP>::LDS;
+    __shared__ __attribute__((aligned(16))) char lds[A > B ? A : B];
+    if ((int)blockIdx.x < nk) dkv_block<T, DP, CAP, BIAS>(g, (int)blockIdx.x, lds);
+    else dq_block<T, DP, CAP, BIAS>(g, (int)blockIdx.x - nk, lds);
+}
+
 // ------------------------------------------------------------- launches
 template <typename T, int DP, bool CAP, bool BIAS> void launch_fwd(const StreamArgs& a, bool few, hipStream_t st) {
     const int64_t rows = (int64_t)a.J * a.pack, nz = (int64_t)a.B * (a.H / a.pack) * a.splits;
@@ -1230,12 +1257,17 @@ template <typename T, int DP, bool CAP, bool BIAS> void launch_fwd(const StreamA
 template <typename T, int DP, bool CAP, bool BIAS> void launch_bwd(const StreamArgs& a, hipStream_t st) {
     const int64_t nk = (int64_t)((a.K + STREAM_KEYS - 1) / STREAM_KEYS) * a.B * a.G;
     const int64_t nq = (int64_t)((a.J + 127) / 128) * a.B * a.H;
-    if (nk > 0) dkv_k<T, DP, CAP, BIAS><<<dim3((unsigned)(nk * a.hparts)), NT, 0, st>>>(a);
-    if (nk > 0 && a.hparts > 1) {
+    const int64_t nkb = nk * a.hparts;
+    if (DP <= 64 || nkb + nq <= STREAM_BOTH) {
+        dkv_dq_k<T, DP, CAP, BIAS><<<dim3((unsigned)(nkb + nq)), NT, 0, st>>>(a, (int)nkb);
+    } else if constexpr (DP > 64) {
+        if (nkb > 0) dkv_k<T, DP, CAP, BIAS><<<dim3((unsigned)nkb), NT, 0, st>>>(a);
+        if (nq > 0) dq_k<T, DP, CAP, BIAS><<<dim3((unsigned)nq), NT, 0, st>>>(a);
+    }
+    if (a.hparts > 1) {
         const int64_t n = (int64_t)a.B * a.G * a.K * (2 * a.P / 8);
         dkv_join_k<T><<<dim3((unsigned)((n + NT - 1) / NT)), NT, 0, st>>>(a);
     }
-    if (nq > 0) dq_k<T, DP, CAP, BIAS><<<dim3((unsigned)nq), NT, 0, st>>>(a);
 }
 
 // fn(head size, capped, biased) as compile-time values
