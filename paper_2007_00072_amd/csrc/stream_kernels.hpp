@@ -771,19 +771,25 @@ template <typename T> __device__ __forceinline__ void hold_overflow(bool on) {
 // dK and dV of 128 keys (32 a wave) of one key/value head: walks the query
 // rows of its query heads (of a part of them where the heads are split),
 // 64 a step.
-template <typename T, int DP> struct DkvTiles {
+// QH = 1: 4 waves, each with its keys' K and V in registers.
+// QH = 2, head sizes above 64: there the sums' registers alone leave one wave
+// a SIMD, which waits for LDS half of its time; so 8 waves, of which two
+// share 32 keys and take half a step's rows each, K and V in LDS, and the
+// pairs' sums meet at the end.
+template <typename T, int DP, int QH> struct DkvTiles {
     static constexpr int BQ = 64, TB = BQ * Tile<T, DP>::PITCH;
+    static constexpr int KT = QH == 2 ? STREAM_KEYS * Tile<T, DP>::PITCH : 0;  // of K, and of V
     // tiles of q and dout, and the rows' numbers: -lse, -D, bounds, documents
     static constexpr int STEP = 2 * TB + BQ * 16;
     static constexpr int NB = 2 * STEP <= 131072 + 4096 ? 2 : 1;
-    static constexpr int LDS = NB * STEP;
+    static constexpr int LDS = 2 * KT + NB * STEP;
 };
-template <typename T, int DP, bool CAP, bool BIAS>
+template <typename T, int DP, bool CAP, bool BIAS, int QH>
 __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* lds) {
-    constexpr int BQ = 64, ND = DP / 32, NC = DP / 16;
-    constexpr bool FRAGS = sizeof(T) == 2;
+    constexpr int BQ = 64, ND = DP / 32, NC = DP / 16, LANES = NT * QH;
+    constexpr bool FRAGS = sizeof(T) == 2 && QH == 1;
     using TL = Tile<T, DP>;
-    using Tiles = DkvTiles<T, DP>;
+    using Tiles = DkvTiles<T, DP, QH>;
     constexpr int TB = Tiles::TB, STEP = Tiles::STEP, NB = Tiles::NB;
     int tile, z;
     place(block, g.B * g.G * g.hparts, tile, z);
@@ -791,7 +797,7 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
     z /= g.hparts;
     const int b = z / g.G, kvh = z - b * g.G, grp = g.H / g.G, k0 = tile * STREAM_KEYS;
     const int tid = threadIdx.x, lane = tid & 63, c32 = lane & 31, hh = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int w8 = __builtin_amdgcn_readfirstlane(tid >> 6), wave = QH == 2 ? w8 & 3 : w8, qh = QH == 2 ? w8 >> 2 : 0;
     const Seq sq(g, b);
     const int32_t* docs = g.doc ? g.doc + (int64_t)b * g.K : nullptr;
     const int key = k0 + 32 * wave + c32;
@@ -800,17 +806,34 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
     const Scorer<T, CAP, BIAS> sc(g);
     const Gain gn = gain<T>(g, b, kvh);
 
-    Frag<T> kf[NC], vf[NC];
-    {
-        const T* kp = reinterpret_cast<const T*>(g.k.ptr) + b * g.k.sb + kvh * g.k.sh + (int64_t)key * g.k.st;
-        const T* vp = reinterpret_cast<const T*>(g.v.ptr) + b * g.v.sb + kvh * g.v.sh + (int64_t)key * g.v.st;
+    const T* kp = reinterpret_cast<const T*>(g.k.ptr) + b * g.k.sb + kvh * g.k.sh;
+    const T* vp = reinterpret_cast<const T*>(g.v.ptr) + b * g.v.sb + kvh * g.v.sh;
+    Frag<T> kr_[QH == 1 ? NC : 1], vr_[QH == 1 ? NC : 1];
+    if constexpr (QH == 1) {
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int e = 16 * c + 8 * hh;
-            kf[c] = kin && e < g.P ? frag_load<T>(kp + e) : frag_zero<T>();
-            vf[c] = kin && e < g.P ? frag_load<T>(vp + e) : frag_zero<T>();
+            kr_[c] = kin && e < g.P ? frag_load<T>(kp + (int64_t)key * g.k.st + e) : frag_zero<T>();
+            vr_[c] = kin && e < g.P ? frag_load<T>(vp + (int64_t)key * g.v.st + e) : frag_zero<T>();
         }
+    } else {
+        Copies<T, DP, STREAM_KEYS, LANES> c;
+        auto in = [&](int r) { return k0 + r < sq.k_len && docs[k0 + r] >= 0; };
+        c.init(tid, g.P, g.k.st);
+        c.issue(tid, reinterpret_cast<const char*>(kp + (int64_t)k0 * g.k.st), sq.k_len - k0, lds_offset(lds), !docs, in);
+        c.init(tid, g.P, g.v.st);
+        c.issue(tid, reinterpret_cast<const char*>(vp + (int64_t)k0 * g.v.st), sq.k_len - k0, lds_offset(lds) + Tiles::KT,
+                !docs, in);
     }
+    auto kf = [&](int c) {
+        if constexpr (QH == 1) return kr_[c];
+        else return TL::row(lds, 32 * wave + c32, 16 * c + 8 * hh);
+    };
+    auto vf = [&](int c) {
+        if constexpr (QH == 1) return vr_[c];
+        else return TL::row(lds + Tiles::KT, 32 * wave + c32, 16 * c + 8 * hh);
+    };
+    char* const steps = lds + 2 * Tiles::KT;
     floatx16 dk[ND], dv[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -858,11 +881,11 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
         return nst;
     };
 
-    Copies<T, DP, BQ> cq, cd;
+    Copies<T, DP, BQ, LANES> cq, cd;
     cq.init(tid, g.P, g.q.st);
     cd.init(tid, g.P, g.dout.st);
-    const uint32_t base = lds_offset(lds);
-    auto rows_of = [&](int buf) { return reinterpret_cast<float*>(lds + buf * STEP + 2 * TB); };
+    const uint32_t base = lds_offset(steps);
+    auto rows_of = [&](int buf) { return reinterpret_cast<float*>(steps + buf * STEP + 2 * TB); };
     hold_overflow<T>(true);
     const int h_end = min(grp, (part + 1) * ((grp + g.hparts - 1) / g.hparts));
     for (int hg = part * ((grp + g.hparts - 1) / g.hparts); hg < h_end; ++hg) {
@@ -910,12 +933,13 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
             const int j0 = s * BQ;
             // (rows behind the last query have zeros and no probabilities)
             const bool some = k0 + 32 * wave + 32 > sq.hi(g, j0) || (docs && !win.is(win.whole, s));
-            const char *tq = lds + buf * STEP, *td = tq + TB;
+            const char *tq = steps + buf * STEP, *td = tq + TB;
             const float* rows = rows_of(buf);
             s = next(s + 1);
             if (NB == 2 && s < nst) fetch(s, buf ^ 1);
 #pragma unroll
-            for (int n = 0; n < BQ / 32; ++n) {
+            for (int n0 = 0; n0 < BQ / 32; n0 += QH) {
+                const int n = QH == 2 ? qh : n0;
                 floatx16 x, dpd;
                 float nl[16];
 #pragma unroll
@@ -931,8 +955,8 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
                 }
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
-                    x = mma<T>(TL::row(tq, 32 * n + c32, 16 * c + 8 * hh), kf[c], x);
-                    dpd = mma<T>(TL::row(td, 32 * n + c32, 16 * c + 8 * hh), vf[c], dpd);
+                    x = mma<T>(TL::row(tq, 32 * n + c32, 16 * c + 8 * hh), kf(c), x);
+                    dpd = mma<T>(TL::row(td, 32 * n + c32, 16 * c + 8 * hh), vf(c), dpd);
                 }
                 // (the second products' fragments are asked for ahead of the
                 // exponentials, which hide the reads)
@@ -990,8 +1014,30 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
             }
         }
     }
-    if (key >= g.K) return;
     hold_overflow<T>(false);
+    if constexpr (QH == 2) {
+        __syncthreads();
+        float* sum = reinterpret_cast<float*>(lds) + (wave * 32 * ND) * 64 + lane;
+        if (qh == 1) {
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    sum[(32 * d + i) * 64] = dk[d][i];
+                    sum[(32 * d + 16 + i) * 64] = dv[d][i];
+                }
+        }
+        __syncthreads();
+        if (qh == 1) return;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                dk[d][i] += sum[(32 * d + i) * 64];
+                dv[d][i] += sum[(32 * d + 16 + i) * 64];
+            }
+    }
+    if (key >= g.K) return;
     const float fk = g.scaler * sc.SLOPE * gn.dsinv;
     T* dkp = reinterpret_cast<T*>(g.dk.ptr) + b * g.dk.sb + kvh * g.dk.sh + (int64_t)key * g.dk.st;
     T* dvp = reinterpret_cast<T*>(g.dv.ptr) + b * g.dv.sb + kvh * g.dv.sh + (int64_t)key * g.dv.st;
@@ -1165,37 +1211,40 @@ __device__ __forceinline__ void dq_block(const StreamArgs& g, int block, char* l
                 x = mma<T>(TL::row(tk, 32 * n + c32, 16 * c + 8 * hh), qf[c], x);
                 dpd = mma<T>(TL::row(tv, 32 * n + c32, 16 * c + 8 * hh), df[c], dpd);
             }
-            float p[16], ds[16];
+            // 16 keys at a time: the second 16's exponentials run beside the
+            // first's products, and fewer values are held at once
             const float far = BIAS ? (float)(pos - k0 - 32 * n - 4 * hh) : 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float v = sc.value(x[i]);
-                float e = fmaf(v, sc.scale, nl);
-                if constexpr (BIAS) e = fmaf(-slope2, fabsf(far - (float)(8 * (i >> 2) + (i & 3))), e);
-                p[i] = __builtin_amdgcn_exp2f(e);
-                ds[i] = CAP ? dpd[i] * sc.slope(v) : dpd[i];
-            }
-            if (mixed) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int4 kd = *reinterpret_cast<const int4*>(kdoc + buf * BN + 32 * n + 8 * q + 4 * hh);
-                    const int id[4] = {kd.x, kd.y, kd.z, kd.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (id[i] != mydoc) p[4 * q + i] = 0.f;
-                }
-            }
-            if (k0 + BN > hi_low) {
-                const int end = hi - k0 - 32 * n - 4 * hh;
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (8 * (i >> 2) + (i & 3) >= end) p[i] = 0.f;
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) ds[i] = score_grad<T>(p[i], ds[i], gn);
+            const int end = hi - k0 - 32 * n - 4 * hh;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const Frag<T> sf = frag_acc<T>(ds + 8 * c);
+                float p[8], ds[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int r = 16 * c + 8 * (i >> 2) + (i & 3);
+                    const float v = sc.value(x[8 * c + i]);
+                    float e = fmaf(v, sc.scale, nl);
+                    if constexpr (BIAS) e = fmaf(-slope2, fabsf(far - (float)r), e);
+                    p[i] = __builtin_amdgcn_exp2f(e);
+                    ds[i] = CAP ? dpd[8 * c + i] * sc.slope(v) : dpd[8 * c + i];
+                }
+                if (mixed) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const int4 kd = *reinterpret_cast<const int4*>(kdoc + buf * BN + 32 * n + 16 * c + 8 * q + 4 * hh);
+                        const int id[4] = {kd.x, kd.y, kd.z, kd.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (id[i] != mydoc) p[4 * q + i] = 0.f;
+                    }
+                }
+                if (k0 + BN > hi_low) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (16 * c + 8 * (i >> 2) + (i & 3) >= end) p[i] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ds[i] = score_grad<T>(p[i], ds[i], gn);
+                const Frag<T> sf = frag_acc<T>(ds);
 #pragma unroll
                 for (int d = 0; d < ND; ++d) dq[d] = mma<T>(TL::col(tk, 32 * n + 16 * c, 32 * d, lane), sf, dq[d]);
             }
@@ -1225,10 +1274,11 @@ __device__ __forceinline__ void dq_block(const StreamArgs& g, int block, char* l
         }
 }
 
-template <typename T, int DP, bool CAP, bool BIAS>
-__global__ __launch_bounds__(NT) void dkv_k(StreamArgs g) {
-    __shared__ __attribute__((aligned(16))) char lds[DkvTiles<T, DP>::LDS];
-    dkv_block<T, DP, CAP, BIAS>(g, (int)blockIdx.x, lds);
+template <typename T, int DP, bool CAP, bool BIAS, int QH>
+__global__ __launch_bounds__(NT * QH) void dkv_k(StreamArgs g) {
+    __shared__ __attribute__((aligned(16))) char lds[DkvTiles<T, DP, QH>::LDS];
+    static_assert(QH == 1 || DkvTiles<T, DP, QH>::LDS >= DP * 1024, "the pairs' sums");
+    dkv_block<T, DP, CAP, BIAS, QH>(g, (int)blockIdx.x, lds);
 }
 template <typename T, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void dq_k(StreamArgs g) {
@@ -1239,9 +1289,9 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void dq_k(StreamArgs g)
 // blocks 0 .. nk - 1 (the longer ones) do keys, the others rows.
 template <typename T, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_dq_k(StreamArgs g, int nk) {
-    constexpr int A = DkvTiles<T, DP>::LDS, B = DqTiles<T, DP>::LDS;
+    constexpr int A = DkvTiles<T, DP, 1>::LDS, B = DqTiles<T, DP>::LDS;
     __shared__ __attribute__((aligned(16))) char lds[A > B ? A : B];
-    if ((int)blockIdx.x < nk) dkv_block<T, DP, CAP, BIAS>(g, (int)blockIdx.x, lds);
+    if ((int)blockIdx.x < nk) dkv_block<T, DP, CAP, BIAS, 1>(g, (int)blockIdx.x, lds);
     else dq_block<T, DP, CAP, BIAS>(g, (int)blockIdx.x - nk, lds);
 }
 
@@ -1261,7 +1311,8 @@ template <typename T, int DP, bool CAP, bool BIAS> void launch_bwd(const StreamA
     if (DP <= 64 || nkb + nq <= STREAM_BOTH) {
         dkv_dq_k<T, DP, CAP, BIAS><<<dim3((unsigned)(nkb + nq)), NT, 0, st>>>(a, (int)nkb);
     } else if constexpr (DP > 64) {
-        if (nkb > 0) dkv_k<T, DP, CAP, BIAS><<<dim3((unsigned)nkb), NT, 0, st>>>(a);
+        constexpr int QH = sizeof(T) == 2 ? 2 : 1;  // (two tiles of float32 keys and rows do not fit LDS together)
+        if (nkb > 0) dkv_k<T, DP, CAP, BIAS, QH><<<dim3((unsigned)nkb), NT * QH, 0, st>>>(a);
         if (nq > 0) dq_k<T, DP, CAP, BIAS><<<dim3((unsigned)nq), NT, 0, st>>>(a);
     }
     if (a.hparts > 1) {

@@ -73,6 +73,18 @@ def test_cap_and_distance(dt, P, cap, alibi):
 
 
 @pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("P", [72, 96, 128])
+def test_many_blocks_of_wide_heads(dt, P):
+    # more blocks than one launch of the backward takes both kernels for
+    B, K, H, G = 12, 301, 16, 8
+    doc = (torch.arange(K) // 140).int().expand(B, K).contiguous()
+    doc[3, 60:75] = -1
+    n = torch.randint(1, K + 1, (B,), generator=torch.Generator().manual_seed(9)).int()
+    compare(dt, B, K, K, H, G, P, causal=True, cap=6.0)
+    compare(dt, B, K, K, H, G, P, doc=doc, k_len=n, q_len=n, slopes=torch.full((H,), 0.05))
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("causal", [False, True])
 def test_documents(dt, causal):
     # documents of 1 to 130 keys, padding inside and behind, ids in no order
