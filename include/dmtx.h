@@ -300,7 +300,7 @@ typedef struct {
     int32_t dtype;           /* dm_dtype of all tensors; scores and sums are fp32, and     */
                              /* probabilities enter the products in the storage type       */
     float scaler;            /* <= 0 selects 1/sqrt(P)                                     */
-    float cap;               /* 0: none                                                    */
+    float cap;               /* 0: none; else from 2^-10 to 2^10                           */
     int32_t causal;          /* 0 or 1                                                     */
     dm_attn_stride q, k, v, out;  /* dq, dk, dv, dout as q, k, v, out                      */
     const int32_t* q_len;    /* device [B] or NULL: J                                      */

@@ -120,9 +120,15 @@ int check_desc(const dm_attn_desc* d) {
         d->K > (1 << 30) || (int64_t)d->H * d->J > INT32_MAX || (int64_t)d->B * d->H > INT32_MAX / 64)
         return set_error(DM_ERR_UNSUPPORTED, "B=%d H=%d G=%d J=%d K=%d: more than 2^31 - 1 rows", d->B, d->H, d->G, d->J,
                          d->K);
-    if (!isfinite(d->scaler) || !isfinite(d->cap) || d->cap < 0.f)
-        return set_error(DM_ERR_ARG, "scaler=%g cap=%g", d->scaler, d->cap);
+    if (!isfinite(d->scaler)) return set_error(DM_ERR_ARG, "scaler=%g", d->scaler);
+    // (the kernels' tanh is off by about 1e-7 of the cap)
+    if (d->cap != 0.f && !(d->cap >= 0x1p-10f && d->cap <= 0x1p10f))
+        return set_error(DM_ERR_ARG, "cap=%g is neither 0 nor from 2^-10 to 2^10", d->cap);
     if (d->causal != 0 && d->causal != 1) return set_error(DM_ERR_ARG, "causal=%d", d->causal);
+    const void* aux[5] = {d->q_len, d->k_len, d->doc, d->prefix, d->slopes};
+    const char* name[5] = {"q_len", "k_len", "doc", "prefix", "slopes"};
+    for (int i = 0; i < 5; ++i)
+        if ((uintptr_t)aux[i] & 3u) return set_error(DM_ERR_ARG, "%s is not 4-byte aligned", name[i]);
     if (d->prefix && !d->causal) return set_error(DM_ERR_ARG, "prefix without causal: every key is seen already");
     DM_TRY(check_stride(d->q, d->J, d->P, "q"));
     DM_TRY(check_stride(d->k, d->K, d->P, "k"));

@@ -737,9 +737,10 @@ __global__ __launch_bounds__(NT) void rows_k(StreamArgs g) {
 }
 
 // fp16: probabilities are held as 2^10 p; score gradients as 2^e ds with
-// 2^e about 1 / max |dout| over the heads of a key/value head, so that they
-// are at most about 2 p sum |v| and keep all their bits down to 6e-5 of
-// that scale; what would pass the type's largest value is held to it.
+// 2^e about 1 / (2 max |dout|) over the heads of a key/value head, so that
+// they are at most p sum |v| (65504, the type's largest value, only where
+// values of 512 agree over a head of 128: such are held to it) and keep all
+// their bits down to 6e-5.
 struct Gain {
     float p2;   // added to the exponents of the probabilities
     float pinv; // 1 / 2^p2
@@ -753,7 +754,7 @@ __device__ __forceinline__ Gain gain(const StreamArgs& g, int b, int kvh) {
     float top = 0.f;
     for (int i = threadIdx.x & 63; i < n; i += 64) top = fmaxf(top, p[i]);
     top = group_max<64>(top);
-    const int e = top > 0.f && top < INFINITY ? -ilogbf(top) : 0;
+    const int e = top > 0.f && top < INFINITY ? -1 - ilogbf(top) : 0;
     return Gain{10.f, 1.f / 1024.f, ldexpf(1.f, e - 10), ldexpf(1.f, -e)};
 }
 // p (dout . v - D), scaled
@@ -1016,6 +1017,7 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
     }
     hold_overflow<T>(false);
     if constexpr (QH == 2) {
+        copied();  // (K and V, where no step waited for them)
         __syncthreads();
         float* sum = reinterpret_cast<float*>(lds) + (wave * 32 * ND) * 64 + lane;
         if (qh == 1) {

@@ -266,6 +266,8 @@ class AdamW:
             state_bits = 32 if m[0].dtype == torch.float32 else 8
         self.params = [_dense("param", p, self.dtype, p.shape, self.device) for p in params]
         self._shapes = [p.shape for p in params]
+        if len({p.data_ptr() for p in params if p.numel()}) < sum(1 for p in params if p.numel()):
+            raise ValueError("a parameter is listed twice")
         if isinstance(master, str):
             master = [p.float() for p in params] if self.dtype != torch.float32 else None
         sd = torch.float32 if state_bits == 32 else torch.float8_e4m3fn

@@ -16,6 +16,15 @@ HP = dict(lr=2e-3, beta1=0.9, beta2=0.99, eps=1e-8)
 SIZES = [1, 3, 255, 256, 257, 4095, 4096, 4097, 10000, 70001]
 
 
+@pytest.fixture(autouse=True)
+def float32_by_default():
+    # (other test modules may have set another default type)
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 def tensors(sizes, seed, std):
     g = torch.Generator().manual_seed(seed)
     return [torch.randn(n, generator=g) * std for n in sizes]

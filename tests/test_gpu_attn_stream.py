@@ -12,6 +12,15 @@ DEV = "cuda"
 T = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
 
 
+@pytest.fixture(autouse=True)
+def float32_by_default():
+    # (other test modules may have set another default type)
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 def normal(seed, *shape, std=1.0):
     return torch.randn(*shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64) * std
 
@@ -82,6 +91,10 @@ def test_many_blocks_of_wide_heads(dt, P):
     n = torch.randint(1, K + 1, (B,), generator=torch.Generator().manual_seed(9)).int()
     compare(dt, B, K, K, H, G, P, causal=True, cap=6.0)
     compare(dt, B, K, K, H, G, P, doc=doc, k_len=n, q_len=n, slopes=torch.full((H,), 0.05))
+    # sequences without queries: their keys have no gradient
+    q, k, v, g = inputs(dt, B, K, K, H, G, P)
+    got = run(q, k, v, g, q_len=torch.zeros(B, dtype=torch.int32))
+    assert not any(t.any() for t in got.values())
 
 
 @pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])

@@ -10,6 +10,15 @@ T = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
 U = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
 
 
+@pytest.fixture(autouse=True)
+def float32_by_default():
+    # (other test modules may have set another default type)
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 def make(dt, tokens, V, I, kind="even", seed=1):
     g = torch.Generator().manual_seed(seed)
     table = torch.randn(V, I, generator=g).to(T[dt])

@@ -10,6 +10,15 @@ from paper_2007_00072_amd import lib, runner
 PTR = 0x10000
 
 
+@pytest.fixture(autouse=True)
+def float32_by_default():
+    # (other test modules may have set another default type)
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 def desc(**kw):
     d = lib.AttnDesc(2, 64, 96, 8, 2, 64, lib.DM_BF16, 0.0, 0.0, 0)
     d.q = d.out = lib.AttnStride(64 * 512, 64, 512)
@@ -22,7 +31,9 @@ def desc(**kw):
 @pytest.mark.parametrize("kw,code,word", [
     (dict(dtype=9), 2, "dtype"), (dict(B=-1), 1, "negative"), (dict(H=7), 1, "multiple"), (dict(G=0), 1, "multiple"),
     (dict(P=60), 2, "head size"), (dict(P=136), 2, "head size"), (dict(cap=-1.0), 1, "cap"),
-    (dict(cap=float("nan")), 1, "cap"), (dict(scaler=float("inf")), 1, "scaler"), (dict(causal=2), 1, "causal"),
+    (dict(cap=float("nan")), 1, "cap"), (dict(cap=1e-4), 1, "cap"), (dict(cap=2000.0), 1, "cap"),
+    (dict(doc=PTR + 2), 1, "doc"), (dict(slopes=PTR + 1), 1, "slopes"),
+    (dict(v=lib.AttnStride(96 * 128, 64, 2 ** 22 + 8)), 2, "v: token"), (dict(k=lib.AttnStride(0, 64, 0)), 2, "k: token"), (dict(scaler=float("inf")), 1, "scaler"), (dict(causal=2), 1, "causal"),
     (dict(prefix=PTR), 1, "prefix"), (dict(J=2 ** 30), 2, "rows"), (dict(K=2 ** 30 + 1), 2, "rows"),
     (dict(k=lib.AttnStride(96 * 128, 64, 132)), 2, "k: strides"), (dict(q=lib.AttnStride(-8, 64, 512)), 2, "negative"),
     (dict(out=lib.AttnStride(0, 64, 512)), 2, "out"), (dict(out=lib.AttnStride(64 * 512, 56, 512)), 2, "overlap"),
@@ -169,6 +180,8 @@ def test_owners_check_their_tensors():
     p = [torch.zeros(3, 4, dtype=f), torch.zeros(5, dtype=f)]
     with pytest.raises(ValueError):
         runner.AdamW([p[0], p[1].float()])
+    with pytest.raises(ValueError):
+        runner.AdamW([p[0], p[1], p[0]])
     with pytest.raises(ValueError):
         runner.AdamW(p).step([torch.zeros(3, 4)], 1)
     with pytest.raises(ValueError):
