@@ -7,7 +7,9 @@
  * (Ivanov, Dryden, Ben-Nun, Li, Hoefler; MLSys 2021).  Index letters follow
  * the paper's problem statement (Fig. 1 caption): P/W key/value projection
  * size, H heads, I embedding size, B batch, J query length, K key/value
- * length.  F (feed-forward width) is this library's letter.
+ * length.  F (feed-forward width) is this library's letter.  Around the layer
+ * it has attention over given q, k, v with masks and score modifiers, the
+ * embedding lookup with its gradient, and an AdamW step.
  *
  * Conventions for every entry point:
  *  - Pointers are DEVICE pointers unless stated otherwise.  The caller owns
