@@ -2,6 +2,8 @@
 // workspace layout and the choice of the forward's form.
 #include <math.h>
 
+#include <algorithm>
+
 #include "checks.hpp"
 #include "stream.hpp"
 
@@ -26,18 +28,25 @@ bool few_rows(const dm_attn_desc& d) {
     return rows <= 2 * STREAM_BM_FEW || blocks * d.K <= 64 * 512;
 }
 
-// Parts the keys are split into, so that the GPU's 256 CUs have two blocks
-// each where the rows alone give fewer, while a part has some steps to walk.
+// Parts the keys are split into where the rows alone give few blocks.
+// Few rows: a block for each of the 256 CUs while a part has two steps to
+// walk, and four (sequences differ in length) while it has eight; a block
+// costs about what five steps do.  (16 sequences of 4096 keys in 8 heads of
+// 64: 4 parts of 8 steps 30 us, 8 of 4 35, 16 of 2 44; 64 of up to 8192 in 4
+// heads of 128: 2 parts 144, 4 132, 8 147.)
+// Otherwise: two blocks for each CU while a part has four steps.
 int key_splits(const dm_attn_desc& d) {
     const bool few = few_rows(d);
     const int64_t bm = few ? STREAM_BM_FEW : STREAM_BM, bn = few ? STREAM_BN_FEW : STREAM_BN;
     const int64_t pack = packed_heads(d);
     const int64_t blocks = ((int64_t)d.J * pack + bm - 1) / bm * d.B * (d.H / pack);
-    const int64_t steps = (d.K + bn - 1) / bn, least = few ? 2 : 4;
-    if (blocks == 0 || blocks >= (few ? 1024 : 384)) return 1;
-    int64_t s = ((few ? 1024 : 512) + blocks - 1) / blocks;
-    if (s > steps / least) s = steps / least;
-    return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+    const int64_t steps = (d.K + bn - 1) / bn;
+    if (blocks == 0) return 1;
+    auto parts = [&](int64_t target, int64_t least) {
+        return blocks >= target ? 1 : std::max<int64_t>(1, std::min((target + blocks - 1) / blocks, steps / least));
+    };
+    const int64_t s = few ? std::max(parts(256, 2), parts(1024, 8)) : blocks >= 384 ? 1 : parts(512, 4);
+    return (int)std::min<int64_t>(s, 64);
 }
 
 // Parts the query heads of a key/value head are split into in the dK / dV

@@ -142,12 +142,18 @@ template <typename T, int DP> struct Tile {
 __device__ __forceinline__ uint32_t lds_offset(const void* p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
 }
-__device__ __forceinline__ void copy16(uint32_t lds, uint32_t voff, u32x4 rsrc) {
+// ONCE: nobody reads these rows again soon, they need not stay in the caches
+template <bool ONCE> __device__ __forceinline__ void copy16(uint32_t lds, uint32_t voff, u32x4 rsrc) {
     // (m0 and the descriptor may come from VALU instructions right before:
     // five wait states to their use)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff),
-                 "s"(rsrc)
-                 : "memory");
+    if constexpr (ONCE)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(lds), "v"(voff),
+                     "s"(rsrc)
+                     : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff),
+                     "s"(rsrc)
+                     : "memory");
 }
 __device__ __forceinline__ void copied() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 // all copies but the last N of this wave
@@ -173,7 +179,7 @@ template <typename T, int DP, int ROWS, int LANES = NT> struct Copies {
         }
     }
     // rows 0 .. left - 1 from `base` into the tile at `lds`; in(r): the row may be read
-    template <typename In>
+    template <bool ONCE = false, typename In>
     __device__ __forceinline__ void issue(int tid, const char* base, int left, uint32_t lds, bool all, In in) const {
         const uint32_t n = (uint32_t)min(max(left, 0), ROWS) * step;
         const u32x4 rsrc{uniform((uint32_t)(uintptr_t)base), uniform((uint32_t)((uintptr_t)base >> 32) & 0xffffu),
@@ -183,7 +189,7 @@ template <typename T, int DP, int ROWS, int LANES = NT> struct Copies {
         for (int i = 0; i < N; ++i) {
             uint32_t v = vo[i];
             if (!all && !in(row(tid, i))) v = NONE;
-            copy16(uniform(to + (uint32_t)i * (LANES * 16)), v, rsrc);
+            copy16<ONCE>(uniform(to + (uint32_t)i * (LANES * 16)), v, rsrc);
         }
     }
 };
@@ -427,8 +433,15 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(S
         const bool all = !docs || !win.is(win.holes, step);
         auto in = [&](int r) { return k0 + r < sq.k_len && docs[k0 + r] >= 0; };
         const uint32_t to = base + (uint32_t)(buf * 2 * RB);
-        ck.issue(who, reinterpret_cast<const char*>(kp + (int64_t)k0 * g.k.st), sq.k_len - k0, to, all, in);
-        cv.issue(who, reinterpret_cast<const char*>(vp + (int64_t)k0 * g.v.st), sq.k_len - k0, to + RB, all, in);
+        const char *kb = reinterpret_cast<const char*>(kp + (int64_t)k0 * g.k.st);
+        const char *vb = reinterpret_cast<const char*>(vp + (int64_t)k0 * g.v.st);
+        if (OWN && nqt == 1) {  // (the only rows that read these keys)
+            ck.template issue<OWN>(who, kb, sq.k_len - k0, to, all, in);
+            cv.template issue<OWN>(who, vb, sq.k_len - k0, to + RB, all, in);
+        } else {
+            ck.issue(who, kb, sq.k_len - k0, to, all, in);
+            cv.issue(who, vb, sq.k_len - k0, to + RB, all, in);
+        }
     };
 
     floatx16 o[ND];
