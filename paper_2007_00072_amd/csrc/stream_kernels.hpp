@@ -318,18 +318,20 @@ __device__ __forceinline__ void place(int lid, int nz, int& tile, int& z) {
 // WQ = 4: the waves share the step's tiles, of which one pair is filled
 // while the other is read.
 // WQ = 1, few rows: reading the keys is what takes time.  Each wave copies
-// its own 32 keys of a step and waits for nobody else; a pair of tiles is
-// asked for as soon as it has been read, so that two steps are on their way
-// whenever the wave waits (with shared tiles, a barrier and one step on its
-// way at a time 165 us where this takes 129: 64 sequences of up to 8192 keys
-// in 4 key/value heads of 128).
+// its own 32 keys of a step and waits for nobody else; tiles are asked for as
+// soon as they have been read.  Two blocks fit a CU (64 KB of LDS, one pair of
+// tiles a wave for heads of 128, two for smaller ones), so that the one's
+// first and last steps lie beside the other's reads.  64 sequences of up to
+// 8192 keys in 4 key/value heads of 128 (538 MB): 115 us, the rate of a large
+// copy; 133 with two pairs of tiles and one block a CU, 165 with tiles that
+// the waves share and a barrier in every step.
 template <typename T, int DP, bool CAP, bool BIAS, int WQ, int NS>
-__global__ __launch_bounds__(NT, sizeof(T) == 2 && WQ == 4 ? 2 : 1) void fwd_k(StreamArgs g) {
+__global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void fwd_k(StreamArgs g) {
     constexpr int WK = 4 / WQ, BM = 32 * WQ, BN = 32 * WK * NS, ND = DP / 32, NC = DP / 16;
     constexpr bool OWN = WK > 1;  // tiles of a wave's own
     using TL = Tile<T, DP>;
     constexpr int TB = BN * TL::PITCH;  // bytes of a step's keys
-    constexpr int NB = 4 * TB <= 131072 ? 2 : 1;
+    constexpr int NB = 4 * TB <= (OWN ? 65536 : 131072) ? 2 : 1;
     constexpr int ROWS = OWN ? 32 * NS : BN, RB = ROWS * TL::PITCH;  // of a tile
     // joining the waves along the keys: m, l and o of all but the first
     constexpr int JOIN = WK > 1 ? (WK - 1) * 64 * (2 + 16 * ND) * 4 : 0;
