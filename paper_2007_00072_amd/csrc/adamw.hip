@@ -80,7 +80,9 @@ __device__ __forceinline__ void load4(const uint8_t* p, int n, float scale, floa
 template <bool ROOT> __device__ __forceinline__ float pack4(uint8_t* p, int n, const float x[4]) {
     const float top = group_max<64>(fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3]))));
     const bool held = top >= LEAST;
-    const float f = held ? E4M3_MAX / top : 0.f;
+    // (both by a reciprocal, as a plain form of it on the device computes them: one ulp of the scale moves codes
+    // that lie next to a tie, and an element whose second moment is tiny turns that into a step of its own)
+    const float f = held ? (1.f / top) * E4M3_MAX : 0.f;
     int r = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * f, x[1] * f, 0, false);
     r = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * f, x[3] * f, r, true);
     uint32_t c = (uint32_t)r;
@@ -96,7 +98,7 @@ template <bool ROOT> __device__ __forceinline__ float pack4(uint8_t* p, int n, c
         for (int i = 0; i < 4; ++i)
             if (i < n) p[i] = (uint8_t)(c >> (8 * i));
     }
-    return held ? top / E4M3_MAX : 0.f;
+    return held ? top * (1.f / E4M3_MAX) : 0.f;
 }
 
 template <typename T, bool MASTER, int BITS>

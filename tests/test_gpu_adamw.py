@@ -223,3 +223,36 @@ def test_writes_stay_inside():
     torch.cuda.synchronize()
     for b, n in bufs:
         assert bool((b[:band] == 0xA5).all()) and bool((b[band + n:] == 0xA5).all())
+
+
+def test_8_bit_states_are_the_plain_forms_bit_for_bit():
+    # every operation rounds by itself in float32, the scale by a reciprocal:
+    # several steps of the same operations by torch give the same codes
+    n, c1, c2 = 256 * 1600, 1 - HP["beta1"], 1 - HP["beta2"]
+    w, m, r, *grads = (t.to(DEV) for t in tensors([n] * 6, 31, 0.02))
+
+    def pack(x, root):
+        top = x.view(-1, 256).abs().amax(1)
+        y = x.view(-1, 256) * (torch.reciprocal(top) * 448.0)[:, None]
+        code = y.to(torch.float8_e4m3fn)
+        if root:
+            code = torch.where((y > 0) & (code.float() == 0), 2.0 ** -9, code.float()).to(torch.float8_e4m3fn)
+        return code.view(-1), top * torch.tensor(1 / 448.0, dtype=torch.float32)
+
+    def value(code, scale):
+        return (code.float().view(-1, 256) * scale[:, None]).view(-1)
+
+    mc, ms = pack(m, False)
+    vc, vs = pack(r.abs(), True)
+    own = [t.clone() for t in (w, mc, vc, ms, vs)]
+    o = runner.AdamW([own[0]], m=[own[1]], v=[own[2]], m_scale=[own[3]], v_scale=[own[4]], decay=[0.0], **HP)
+    for s, g in enumerate(grads):
+        step = 50 + s
+        o.step([g], step)
+        m = value(mc, ms) * HP["beta1"] + g * c1
+        v = value(vc, vs) ** 2 * HP["beta2"] + (g * g) * c2
+        u = (m * (1.0 / (1.0 - HP["beta1"] ** step))) / (torch.sqrt(v * (1.0 / (1.0 - HP["beta2"] ** step))) + HP["eps"])
+        w = w - u * HP["lr"]
+        (mc, ms), (vc, vs) = pack(m, False), pack(torch.sqrt(v), True)
+        for a, b in zip(own, (w, mc, vc, ms, vs)):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
