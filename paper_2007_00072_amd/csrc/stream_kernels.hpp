@@ -155,7 +155,13 @@ template <bool ONCE> __device__ __forceinline__ void copy16(uint32_t lds, uint32
                      "s"(rsrc)
                      : "memory");
 }
-__device__ __forceinline__ void copied() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// (The builtin tells the compiler that its own loads have come as well: else
+// it waits for one from ahead of a loop, a row's q, in every step of the
+// loop, and by then for the copies that were asked for a moment ago.)
+__device__ __forceinline__ void copied() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0) alone
+}
 // all copies but the last N of this wave
 template <int N> __device__ __forceinline__ void copied_but() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 // this wave's LDS reads so far
@@ -486,12 +492,20 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void fwd_k(StreamArgs g
 
         floatx16 a[NS];
 #pragma unroll
-        for (int n = 0; n < NS; ++n) {
+        for (int n = 0; n < NS; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) a[n][i] = 0.f;
+        // (all of K's fragments are asked for ahead of the first product: left
+        // to itself the compiler waits for each right after asking)
+        constexpr int AH = sizeof(T) == 2 && !OWN ? (DP <= 96 ? NS * NC : 12) : 0;
+        Frag<T> kf[AH ? AH : 1];
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
-                a[n] = mma<T>(TL::row(tk, 32 * n + c32, 16 * c + 8 * hh), qf[c], a[n]);
+        for (int i = 0; i < AH; ++i) kf[i] = TL::row(tk, 32 * (i / NC) + c32, 16 * (i % NC) + 8 * hh);
+        if constexpr (AH > 0) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < NS * NC; ++i) {
+            const int n = i / NC, c = i % NC;
+            a[n] = mma<T>(i < AH ? kf[i < AH ? i : 0] : TL::row(tk, 32 * n + c32, 16 * c + 8 * hh), qf[c], a[n]);
         }
         float x[NS][16];
         const float far = BIAS ? (float)(pos - k0 - 4 * hh) : 0.f;
@@ -915,8 +929,8 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
         auto put = [&](int buf) {
             if (tid < BQ) {
                 float* r = rows_of(buf) + tid;
-                r[0] = f_lse;  // less lse, in the score's units without its offset
-                r[BQ] = f_d;
+                r[0] = gn.p2 + sc.offset - f_lse;  // in the score's units without its offset
+                r[BQ] = -f_d;
                 reinterpret_cast<int*>(r)[2 * BQ] = f_hi;
                 reinterpret_cast<int*>(r)[3 * BQ] = f_doc;
             }
@@ -928,8 +942,8 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
             if (tid < BQ) {
                 const int j = j0 + tid;
                 const bool row = j < sq.q_len;
-                f_lse = row ? gn.p2 + sc.offset - g.lse[zr + j] : -INFINITY;
-                f_d = row ? -g.dsum[zr + j] : 0.f;
+                f_lse = row ? g.lse[zr + j] : INFINITY;
+                f_d = row ? g.dsum[zr + j] : 0.f;
                 f_hi = sq.hi(g, j);
                 f_doc = docs ? sq.doc_of(g, b, j) : 0;
             }
@@ -1006,7 +1020,7 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
                         const int hi4[4] = {rh.x, rh.y, rh.z, rh.w}, id4[4] = {rd.x, rd.y, rd.z, rd.w};
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            if (key >= hi4[i] || id4[i] != kd || !kin) p[4 * q + i] = 0.f;
+                            if ((key >= hi4[i]) | (id4[i] != kd) | !kin) p[4 * q + i] = 0.f;
                     }
                 }
 #pragma unroll
@@ -1223,10 +1237,27 @@ __device__ __forceinline__ void dq_block(const StreamArgs& g, int block, char* l
                 x[i] = 0.f;
                 dpd[i] = nd;  // dout . v - D
             }
+            // (fragments asked for ahead of the first product, as the forward does)
+            constexpr int AH = sizeof(T) == 2 ? (DP == 32 ? 4 : DP <= 96 ? 8 : 4) : 0;
+            Frag<T> rf[AH ? AH : 1];
+#pragma unroll
+            for (int i = 0; i < AH; ++i) rf[i] = TL::row(i & 1 ? tv : tk, 32 * n + c32, 16 * (i / 2) + 8 * hh);
+            if constexpr (AH > 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                x = mma<T>(TL::row(tk, 32 * n + c32, 16 * c + 8 * hh), qf[c], x);
-                dpd = mma<T>(TL::row(tv, 32 * n + c32, 16 * c + 8 * hh), df[c], dpd);
+                const bool got = 2 * c < AH;
+                x = mma<T>(got ? rf[got ? 2 * c : 0] : TL::row(tk, 32 * n + c32, 16 * c + 8 * hh), qf[c], x);
+                dpd = mma<T>(got ? rf[got ? 2 * c + 1 : 0] : TL::row(tv, 32 * n + c32, 16 * c + 8 * hh), df[c], dpd);
+            }
+            // (up to 64 the registers hold the second product's fragments too)
+            constexpr bool COLS = sizeof(T) == 2 && DP <= 64;
+            Frag<T> cf[2][COLS ? ND : 1];
+            if constexpr (COLS) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) cf[c][d] = TL::col(tk, 32 * n + 16 * c, 32 * d, lane);
+                __builtin_amdgcn_sched_barrier(0x41f);
             }
             // 16 keys at a time: the second 16's exponentials run beside the
             // first's products, and fewer values are held at once
@@ -1263,7 +1294,8 @@ __device__ __forceinline__ void dq_block(const StreamArgs& g, int block, char* l
                 for (int i = 0; i < 8; ++i) ds[i] = score_grad<T>(p[i], ds[i], gn);
                 const Frag<T> sf = frag_acc<T>(ds);
 #pragma unroll
-                for (int d = 0; d < ND; ++d) dq[d] = mma<T>(TL::col(tk, 32 * n + 16 * c, 32 * d, lane), sf, dq[d]);
+                for (int d = 0; d < ND; ++d)
+                    dq[d] = mma<T>(COLS ? cf[c][COLS ? d : 0] : TL::col(tk, 32 * n + 16 * c, 32 * d, lane), sf, dq[d]);
             }
         }
         if (NB == 2) {

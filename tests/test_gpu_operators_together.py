@@ -109,7 +109,7 @@ def test_packed_documents_between_contractions():
     # sums of up to 256 terms in float32 after sums of 64 and 96: far under 2^-12 of the largest element
     for name, got, want in (("out", out, y), ("dx", dx, X.grad), ("dw", dw, W.grad)):
         err = (got.cpu().double().view(want.shape) - want).abs().max() / want.abs().max()
-        assert float(err) < 2.0 ** -14, name
+        assert float(err.detach()) < 2.0 ** -14, name
 
 
 def test_a_prompt_then_single_tokens():
