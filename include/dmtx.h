@@ -360,8 +360,8 @@ int embed_bwd(int32_t dtype, int64_t tokens, int32_t vocab, int32_t cols, const 
  * overlap.
  * state_bits = 32: m and v are float [n].  state_bits = 8: m holds e4m3 codes
  * (OCP, one byte) of m / m_scale, v those of sqrt(v) / v_scale, with a float
- * scale for each 256 elements, the block's largest value (1 / 448) (zero, and
- * codes of zero, for a block below 2^-100); a root that is not zero keeps at
+ * scale for each 256 elements, the block's largest value times 1 / 448 (zero,
+ * and codes of zero, for a block below 2^-100); a root that is not zero keeps at
  * least the smallest code.  The step itself uses m and v before that
  * rounding.  Zeros in codes and scales are the states of a first step. */
 typedef struct {

@@ -283,6 +283,9 @@ __device__ __forceinline__ int2 wave_range(int id) {
     return int2{__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(hi)};
 }
 
+// Smallest and largest document of each 64 keys, and whether some are of
+// none: what the walks below need of documents, at a 64th of the reads.
+// A launch: 3 us for 4 x 4096 keys.
 template <typename T>
 __global__ __launch_bounds__(64) void ranges_k(StreamArgs g) {
     const int nr = (g.K + STREAM_RANGE - 1) / STREAM_RANGE, b = (int)blockIdx.x / nr, e = (int)blockIdx.x - b * nr;
@@ -322,15 +325,23 @@ __device__ __forceinline__ void place(int lid, int nz, int& tile, int& z) {
 // A block takes 32 WQ query rows; its waves lie WQ along the queries and
 // WK = 4 / WQ along the keys of a step (each wave 32 NS of them).
 // WQ = 4: the waves share the step's tiles, of which one pair is filled
-// while the other is read.
+// while the other is read.  128 rows: with 256 registers a wave holds its 32
+// rows' sums and two waves fit a SIMD, of which one multiplies while the
+// other takes exponentials.  A third pair of tiles in flight changes nothing
+// (126 us with and without, heads of 64); what bounds it are the vector
+// instructions of the softmax and the products' latency, with capped scores
+// the vector unit (68 % busy: an exponential and a reciprocal more for each).
+// 4 x 4096 tokens in documents of about 700, 16 heads of 64: 126 us, 0.40
+// PFLOP/s of the pairs that are seen; 8192 causal tokens, capped, 16 heads of
+// 128: 420 us, 0.65; 500 queries behind up to 4096 keys, 16 heads of 96: 39.
 // WQ = 1, few rows: reading the keys is what takes time.  Each wave copies
 // its own 32 keys of a step and waits for nobody else; tiles are asked for as
 // soon as they have been read.  Two blocks fit a CU (64 KB of LDS, one pair of
 // tiles a wave for heads of 128, two for smaller ones), so that the one's
 // first and last steps lie beside the other's reads.  64 sequences of up to
-// 8192 keys in 4 key/value heads of 128 (538 MB): 115 us, the rate of a large
-// copy; 133 with two pairs of tiles and one block a CU, 165 with tiles that
-// the waves share and a barrier in every step.
+// 8192 keys in 4 key/value heads of 128 (up to 538 MB, all but 5 % of them
+// seen): 105 us, the rate of a large copy; 133 with two pairs of tiles and one
+// block a CU, 165 with tiles that the waves share and a barrier in every step.
 template <typename T, int DP, bool CAP, bool BIAS, int WQ, int NS>
 __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void fwd_k(StreamArgs g) {
     constexpr int WK = 4 / WQ, BM = 32 * WQ, BN = 32 * WK * NS, ND = DP / 32, NC = DP / 16;
@@ -677,7 +688,8 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void fwd_k(StreamArgs g
         }
 }
 
-// Joins the parts that fwd_k left, in their order: 16 lanes a row.
+// Joins the parts that fwd_k left, in their order: 16 lanes a row.  Bound by
+// reading them: 4 parts of 16000 rows of 96, 25 MB, in 6.5 us.
 template <typename T>
 __global__ __launch_bounds__(NT) void join_k(StreamArgs g) {
     const int64_t n = (int64_t)g.B * g.H * g.J, zr = ((int64_t)blockIdx.x * NT + threadIdx.x) >> 4;
@@ -722,6 +734,7 @@ __global__ __launch_bounds__(NT) void join_k(StreamArgs g) {
 // every 256 rows of a head, from which the score gradients get a power of
 // two that keeps them out of the type's subnormal numbers (a probability of
 // 1e-5 times a small gradient would lose its bits there).
+// Bound by reading three tensors: 262144 rows of 64 in bf16, 101 MB, in 20 us.
 template <typename T, int LPR>
 __global__ __launch_bounds__(NT) void rows_k(StreamArgs g) {
     constexpr int RPB = NT / LPR, U = 4;
@@ -806,6 +819,10 @@ template <typename T> __device__ __forceinline__ void hold_overflow(bool on) {
 // a SIMD, which waits for LDS half of its time; so 8 waves, of which two
 // share 32 keys and take half a step's rows each, K and V in LDS, and the
 // pairs' sums meet at the end.
+// Four products of the formula's five are here.  Bound by the registers: dK,
+// dV and the operands allow two waves a SIMD, whose exponentials, conversions
+// and LDS reads hide half of the products.  8192 causal tokens, capped, 16
+// heads of 128 over 4 key/value heads: 785 us, 0.70 PFLOP/s (QH = 1: 975).
 template <typename T, int DP, int QH> struct DkvTiles {
     static constexpr int BQ = 64, TB = BQ * Tile<T, DP>::PITCH;
     static constexpr int KT = QH == 2 ? STREAM_KEYS * Tile<T, DP>::PITCH : 0;  // of K, and of V
@@ -1096,6 +1113,7 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
 }
 
 // Sums of the head parts' dK and dV, in their order: 8 elements a thread.
+// Bound by reading them: 4 parts of 32768 rows of 128, 134 MB, in 24 us.
 template <typename T>
 __global__ __launch_bounds__(NT) void dkv_join_k(StreamArgs g) {
     const int np = 2 * g.P / 8;
@@ -1115,7 +1133,10 @@ __global__ __launch_bounds__(NT) void dkv_join_k(StreamArgs g) {
 }
 
 // dQ of 128 query rows (32 a wave) of one head: walks their keys as the
-// forward does.
+// forward does.  Three products, of which two form the probabilities' and
+// their gradients' sums again: that is the price of writing no J x K tensor
+// and adding nothing atomically.  8192 causal tokens, capped, 16 heads of
+// 128: 575 us, 0.72 PFLOP/s.
 template <typename T, int DP> struct DqTiles {
     static constexpr int BN = 64, TB = BN * Tile<T, DP>::PITCH, NB = 4 * TB <= 131072 ? 2 : 1;
     static constexpr int LDS = 2 * NB * TB + 2 * BN * 4 + 4 * 8;  // tiles, documents of the keys, of the waves' rows
@@ -1335,7 +1356,10 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void dq_k(StreamArgs g)
     dq_block<T, DP, CAP, BIAS>(g, (int)blockIdx.x, lds);
 }
 // Both in one launch, so that the end of the one fills with the other:
-// blocks 0 .. nk - 1 (the longer ones) do keys, the others rows.
+// blocks 0 .. nk - 1 (the longer ones) do keys, the others rows.  4 x 4096
+// tokens in documents of about 700, 16 heads of 64: 345 us, 0.52 PFLOP/s of
+// the seven products; 3 x 1531 causal tokens with distances in fp16, 12 heads
+// of 64: 70.
 template <typename T, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_dq_k(StreamArgs g, int nk) {
     constexpr int A = DkvTiles<T, DP, 1>::LDS, B = DqTiles<T, DP>::LDS;

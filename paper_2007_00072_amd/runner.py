@@ -172,7 +172,9 @@ class Attention:
         if self._strides.get(name) != s:
             if s[3] != 1:
                 raise ValueError(f"{name}: the last axis is not contiguous")
-            setattr(self.desc, name, lib.AttnStride(s[0], s[2], s[1]))
+            # (the stride of an axis of one element is never taken: torch has any value there)
+            b, j, h = (x if n > 1 else t.shape[3] for x, n in zip(s, t.shape[:3]))
+            setattr(self.desc, name, lib.AttnStride(b, h, j))
             self._strides[name] = s
 
     def _like(self, name, t, of):
@@ -221,6 +223,7 @@ class Embedding:
         self.scale, self.pad_id = scale, pad_id
         self.grad = torch.empty(table.shape, dtype=torch.float32, device=table.device)
         self.ws = torch.empty(0, dtype=torch.uint8, device=table.device)
+        self._outgrown = []  # workspaces that a captured backward may still use
 
     def forward(self, ids: torch.Tensor, y: Optional[torch.Tensor] = None) -> torch.Tensor:
         V, I = self.table.shape
@@ -238,7 +241,8 @@ class Embedding:
         _dense("dy", dy, self.table.dtype, (*ids.shape, I), self.device)
         need = lib.embed_ws_bytes(ids.numel(), V, I)
         if self.ws.numel() < need:
-            self.ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            self._outgrown.append(self.ws)
+            self.ws = torch.empty(max(need, 2 * self.ws.numel()), dtype=torch.uint8, device=self.device)
         _launch(self.device, lib.embed_bwd, self.code, ids.numel(), V, I, ids, self.pad_id, dy, self.scale,
                 self.grad, self.ws, self.ws.numel())
         return self.grad
@@ -296,12 +300,13 @@ class AdamW:
                    [p.numel() for p in params], decay, strict=True)
         self._items = (lib.AdamwTensor * len(params))(
             *[lib.AdamwTensor(*[lib.ptr(t) for t in r[:7]], *r[7:]) for r in rows])
+        self.lr = lr
         self.desc = lib.AdamwDesc(_code(self.dtype), state_bits, lr, beta1, beta2, eps, 1.0, 0, None)
 
     def step(self, grads: Sequence[torch.Tensor], step: int, lr: Optional[float] = None, grad_scale: float = 1.0,
              scalars: Optional[torch.Tensor] = None) -> None:
         """Step number `step` (1 for the first) with fp32 gradients shaped like
-        the parameters.  scalars: float32 [4] on the device (see adamw_step),
+        the parameters; lr: this step's, in place of self.lr.  scalars: float32 [4] on the device (see adamw_step),
         in place of step, lr and grad_scale."""
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
@@ -314,6 +319,5 @@ class AdamW:
             _dense("scalars", scalars, torch.float32, (4,), self.device)
         d = self.desc
         d.step, d.grad_scale, d.scalars = step, grad_scale, lib.ptr(scalars)
-        if lr is not None:
-            d.lr = lr
+        d.lr = self.lr if lr is None else lr
         _launch(self.device, lib.adamw_step, d, self._items, len(self.params))

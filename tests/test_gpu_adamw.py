@@ -256,3 +256,14 @@ def test_8_bit_states_are_the_plain_forms_bit_for_bit():
         (mc, ms), (vc, vs) = pack(m, False), pack(torch.sqrt(v), True)
         for a, b in zip(own, (w, mc, vc, ms, vs)):
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_learning_rate_of_one_step():
+    w = tensors([300], 7, 0.1)[0].to(DEV)
+    o = runner.AdamW([w], **HP)
+    before, g = w.clone(), torch.ones(300, device=DEV)
+    o.step([g], 1, lr=0.0)
+    assert torch.equal(w, before)
+    o.step([g], 2)
+    # (the second of two equal gradients: a step of about lr)
+    assert ((before - w) / HP["lr"] - 1).abs().max() < 1e-3

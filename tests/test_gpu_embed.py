@@ -136,3 +136,22 @@ def test_writes_stay_inside(tokens):
     torch.cuda.synchronize()
     for b in bufs:
         assert bool((b[:band] == 0xA5).all()) and bool((b[b.numel() - band:] == 0xA5).all())
+
+
+def test_a_captured_backward_outlives_a_larger_one():
+    # (the larger one needs another workspace; the graph keeps its own)
+    table, dy, ids = (t.to(DEV) for t in make("f16", 2000, 2000, 64, "words"))
+    e = runner.Embedding(table)
+    want = e.backward(ids, dy).clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        e.backward(ids, dy)
+    big = [t.to(DEV) for t in make("f16", 30000, 2000, 64, "words", seed=3)]
+    large = e.backward(big[2], big[1]).clone()
+    others = [torch.full((1 << 20,), -1, dtype=torch.int32, device=DEV) for _ in range(8)]
+    for _ in range(2):
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(e.grad, want)
+        assert torch.equal(e.backward(big[2], big[1]), large)
+    assert all((t == -1).all() for t in others)

@@ -187,3 +187,13 @@ def test_owners_check_their_tensors():
     with pytest.raises(ValueError):
         runner.AdamW(p).step([torch.zeros(3, 4), torch.zeros(6)], 1)
     assert C.sizeof(lib.AttnDesc) == 10 * 4 + 12 * 8 + 5 * 8
+
+
+def test_strides_of_axes_of_one_element_are_free():
+    x = torch.zeros(4096, dtype=torch.bfloat16)
+    q = x.as_strided((1, 1, 4, 64), (3, 5, 64, 1))
+    k = x.as_strided((1, 7, 1, 64), (1, 64, 1, 1))
+    runner.Attention(q, k, k)
+    two = x.as_strided((2, 7, 1, 64), (3, 64, 1, 1))
+    with pytest.raises(lib.DmError):
+        runner.Attention(q.expand(2, 1, 4, 64), two, two)
