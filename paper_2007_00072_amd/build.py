@@ -98,7 +98,7 @@ def build(jobs: int = 4, verbose: bool = False, incremental: bool = False) -> st
 # Host-side AddressSanitizer + UndefinedBehaviorSanitizer build of the
 # same sources, for checking the host code (argument validation, workspace
 # carving, plan objects) on a machine without a GPU.  The sanitizers apply
-# to host code only; device code is compiled unoptimised (its kernels are
+# to host code only; device code is hardly optimised (its kernels are
 # never launched from this build).  Load it with the sanitizer runtime
 # preloaded (hostsan_runtime()) and DMTX_LIB pointing at it.
 HOSTSAN_DIR = os.path.join(BUILD, "hostsan")
@@ -140,9 +140,9 @@ def build_hostsan(jobs: int = 4, verbose: bool = False) -> str:
 
     def one(src):
         obj = os.path.join(HOSTSAN_DIR, os.path.splitext(src)[0] + ".o")
-        # (gemm_wide's asm operands are constants and scalar registers only
-        # once its helpers are inlined)
-        opt = "-O1" if src == "gemm_wide.hip" else "-O0"
+        # (the asm operands of these are constants and scalar registers only
+        # once their helpers are inlined)
+        opt = "-O1" if src == "gemm_wide.hip" or src.startswith("stream_") else "-O0"
         cmd = [hipcc(), *HOSTSAN_FLAGS, "-Xarch_device", opt, "-c", os.path.join(CSRC, src), "-o", obj]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
