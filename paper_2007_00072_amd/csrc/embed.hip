@@ -8,6 +8,14 @@ namespace {
 
 constexpr int NT = 256;
 
+// A grid holds less than 2^32 threads along x (more wrap, without an error):
+// more blocks go in several rows, whose last may have blocks without work.
+constexpr int64_t GRID_ROW = (int64_t)1 << 22;
+dim3 rows_of_blocks(int64_t n) {
+    return dim3((unsigned)std::min(n, GRID_ROW), (unsigned)((n + GRID_ROW - 1) / GRID_ROW));
+}
+__device__ __forceinline__ int64_t block_of_rows() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // y[t] = scale table[ids[t]]: `lanes` lanes a token (a power of two), 16
 // bytes of the storage type each at a time.  Bound by memory: 16384 tokens of
 // 1024 in fp16, 34 MB read and 34 written, in 13.5 us.
@@ -15,7 +23,7 @@ template <typename T>
 __global__ __launch_bounds__(NT) void embed_fwd_k(int64_t tokens, int vocab, int cols, int lanes, const int32_t* ids,
                                                   const T* table, float scale, T* y) {
     const int tpb = NT / lanes, gl = threadIdx.x & (lanes - 1);
-    const int64_t t = (int64_t)blockIdx.x * tpb + threadIdx.x / lanes;
+    const int64_t t = block_of_rows() * tpb + threadIdx.x / lanes;
     if (t >= tokens) return;
     const int id = ids[t];
     const bool in = id >= 0 && id < vocab;
@@ -340,7 +348,7 @@ template <typename T, int PC>
 __global__ __launch_bounds__(NT) void sum_k(SumArgs g) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int pieces = (g.tokens + PC - 1) / PC, slabs = (g.cols + 511) / 512;
-    const int64_t id = (int64_t)blockIdx.x * (NT / 64) + wave;
+    const int64_t id = block_of_rows() * (NT / 64) + wave;
     if (id >= (int64_t)pieces * slabs) return;
     const int piece = (int)(id / slabs), col = (int)(id - (int64_t)piece * slabs) * 512 + lane * 8;
     const bool in = col < g.cols;
@@ -412,7 +420,7 @@ __global__ __launch_bounds__(NT) void sum_k(SumArgs g) {
 __global__ __launch_bounds__(NT) void join_parts_k(SumArgs g) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int pieces = (g.tokens + PIECE - 1) / PIECE, slabs = (g.cols + 255) / 256;
-    const int64_t id = (int64_t)blockIdx.x * (NT / 64) + wave;
+    const int64_t id = block_of_rows() * (NT / 64) + wave;
     if (id >= (int64_t)pieces * slabs) return;
     const int piece = (int)(id / slabs);
     const int col = (int)(id - (int64_t)piece * slabs) * 256 + lane * 4;
@@ -475,11 +483,11 @@ template <typename T>
 void launch_sums(const SumArgs& a, hipStream_t st) {
     const int64_t pc = a.part ? PIECE : PIECE_FEW;
     const int64_t waves = (a.tokens + pc - 1) / pc * ((a.cols + 511) / 512);
-    const dim3 grid((unsigned)((waves + NT / 64 - 1) / (NT / 64)));
+    const dim3 grid = rows_of_blocks((waves + NT / 64 - 1) / (NT / 64));
     if (a.part) {
         sum_k<T, PIECE><<<grid, NT, 0, st>>>(a);
         const int64_t joins = (a.tokens + pc - 1) / pc * ((a.cols + 255) / 256);
-        join_parts_k<<<dim3((unsigned)((joins + NT / 64 - 1) / (NT / 64))), NT, 0, st>>>(a);
+        join_parts_k<<<rows_of_blocks((joins + NT / 64 - 1) / (NT / 64)), NT, 0, st>>>(a);
     } else {
         sum_k<T, PIECE_FEW><<<grid, NT, 0, st>>>(a);
     }
@@ -500,8 +508,8 @@ void launch_fwd(int64_t tokens, int vocab, int cols, const int32_t* ids, const v
     int lanes = 1;
     while (lanes < 64 && lanes * 8 < cols) lanes *= 2;
     const int64_t tpb = NT / lanes;
-    embed_fwd_k<T><<<dim3((unsigned)((tokens + tpb - 1) / tpb)), NT, 0, st>>>(tokens, vocab, cols, lanes, ids,
-                                                                             (const T*)table, scale, (T*)y);
+    embed_fwd_k<T><<<rows_of_blocks((tokens + tpb - 1) / tpb), NT, 0, st>>>(tokens, vocab, cols, lanes, ids,
+                                                                           (const T*)table, scale, (T*)y);
 }
 }  // namespace
 }  // namespace dm
