@@ -288,9 +288,9 @@ int residual_add(int32_t dtype, int64_t n, const void* a, const void* b, void* o
  * nothing is summed by atomics. */
 
 /* Element (b, head, token, d) sits at b*b + head*h + token*t + d elements;
- * strides are multiples of 8, not negative, t from P to 2^22, and those of
- * written tensors do not overlap (b and h of k and v that are only read may
- * be 0). */
+ * strides are multiples of 8, not negative, t from P to 2^22 (an axis of one
+ * token: any), and those of written tensors do not overlap (b and h of k and
+ * v that are only read may be 0). */
 typedef struct {
     int64_t b, h, t;
 } dm_attn_stride;

@@ -146,7 +146,11 @@ int check_desc(const dm_attn_desc* d) {
     return check_written(d->out, d->B, d->H, d->J, d->P, "out");
 }
 
-StreamRows rows_of(const void* p, const dm_attn_stride& s) { return {(char*)p, s.b, s.h, s.t}; }
+// (The copies end a step's rows behind the last by the token stride: an axis
+// of one token, which never takes a step, gets a row's own size.)
+StreamRows rows_of(const void* p, const dm_attn_stride& s, int tokens, int P) {
+    return {(char*)p, s.b, s.h, tokens > 1 ? s.t : P};
+}
 
 StreamArgs args_of(const dm_attn_desc& d) {
     StreamArgs a{};
@@ -191,7 +195,8 @@ int attn_fwd(const dm_attn_desc* d, const void* q, const void* k, const void* v,
     if (ws_bytes < s.fwd) return set_error(DM_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws_bytes, s.fwd);
     if (s.fwd) DM_TRY(check_ptr(ws, "ws"));
     StreamArgs a = args_of(*d);
-    a.q = rows_of(q, d->q); a.k = rows_of(k, d->k); a.v = rows_of(v, d->v); a.o = rows_of(out, d->out);
+    a.q = rows_of(q, d->q, d->J, d->P); a.o = rows_of(out, d->out, d->J, d->P);
+    a.k = rows_of(k, d->k, d->K, d->P); a.v = rows_of(v, d->v, d->K, d->P);
     if (saved) {
         a.lse = (float*)saved;
         if (d->dtype != DM_F32) a.lo = (char*)saved + s.lo;
@@ -227,8 +232,10 @@ int attn_bwd(const dm_attn_desc* d, const void* q, const void* k, const void* v,
     if (ws_bytes < s.bwd) return set_error(DM_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws_bytes, s.bwd);
     if (s.bwd) DM_TRY(check_ptr(ws, "ws"));
     StreamArgs a = args_of(*d);
-    a.q = rows_of(q, d->q); a.k = rows_of(k, d->k); a.v = rows_of(v, d->v); a.o = rows_of(out, d->out);
-    a.dout = rows_of(dout, d->out); a.dq = rows_of(dq, d->q); a.dk = rows_of(dk, d->k); a.dv = rows_of(dv, d->v);
+    a.q = rows_of(q, d->q, d->J, d->P); a.o = rows_of(out, d->out, d->J, d->P);
+    a.k = rows_of(k, d->k, d->K, d->P); a.v = rows_of(v, d->v, d->K, d->P);
+    a.dout = rows_of(dout, d->out, d->J, d->P); a.dq = rows_of(dq, d->q, d->J, d->P);
+    a.dk = rows_of(dk, d->k, d->K, d->P); a.dv = rows_of(dv, d->v, d->K, d->P);
     a.lse = (float*)saved;
     if (d->dtype != DM_F32) a.lo = (char*)saved + s.lo;
     a.ranges = (int4*)ws;
