@@ -284,7 +284,8 @@ int residual_add(int32_t dtype, int64_t n, const void* a, const void* b, void* o
  * One entry point covers training, prompts and single tokens (J = 1 over a
  * cache of K keys, of which sequence b holds k_len[b]).
  * The descriptor's device arrays are read by the call's kernels.  Sizes may
- * be 0 (B, J: nothing to do; K: zeros).  Results do not depend on the run:
+ * be 0 (B, J: nothing to do; K: zeros); those that a launch has no blocks
+ * for (B*H of 2^24, say) are refused.  Results do not depend on the run:
  * nothing is summed by atomics. */
 
 /* Element (b, head, token, d) sits at b*b + head*h + token*t + d elements;

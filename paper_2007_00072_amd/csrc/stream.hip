@@ -60,6 +60,25 @@ int head_parts(const dm_attn_desc& d) {
     return (int)(want < grp ? want : grp);
 }
 
+// A grid holds less than 2^32 threads along x (more wrap, without an error).
+constexpr int64_t GRID_THREADS = ((int64_t)1 << 32) - 1;
+
+// Threads of the forward's launches: row tiles, ranges of documents.  (The
+// parts are joined only where there are few rows.)
+bool forward_fits(const dm_attn_desc& d) {
+    const int64_t bm = few_rows(d) ? STREAM_BM_FEW : STREAM_BM, pack = packed_heads(d);
+    const int64_t blocks = ((int64_t)d.J * pack + bm - 1) / bm * d.B * (d.H / pack) * key_splits(d);
+    const int64_t ranges = d.doc ? ((int64_t)d.K + STREAM_RANGE - 1) / STREAM_RANGE * d.B : 0;
+    return blocks * 256 <= GRID_THREADS && ranges * 64 <= GRID_THREADS;
+}
+// Of the backward's: key tiles (wide heads: 512 threads each) and row tiles,
+// in one launch or two; the row terms' blocks are fewer than the row tiles.
+bool backward_fits(const dm_attn_desc& d) {
+    const int64_t keys = ((int64_t)d.K + STREAM_KEYS - 1) / STREAM_KEYS * d.B * d.G * head_parts(d);
+    const int64_t rows = ((int64_t)d.J + STREAM_BM - 1) / STREAM_BM * d.B * d.H;
+    return (keys * (d.P > 64 ? 2 : 1) + rows) * 256 <= GRID_THREADS;
+}
+
 struct Sizes {
     size_t lo, saved;                     // saved: lse, then lo
     size_t ranges, part_o, part_ml, fwd;  // forward workspace: ends of its parts
@@ -129,6 +148,8 @@ int check_desc(const dm_attn_desc* d) {
         d->K > (1 << 30) || (int64_t)d->H * d->J > INT32_MAX || (int64_t)d->B * d->H > INT32_MAX / 64)
         return set_error(DM_ERR_UNSUPPORTED, "B=%d H=%d G=%d J=%d K=%d: more than 2^31 - 1 rows", d->B, d->H, d->G, d->J,
                          d->K);
+    if (!forward_fits(*d))
+        return set_error(DM_ERR_UNSUPPORTED, "B=%d H=%d J=%d K=%d: more blocks than a launch holds", d->B, d->H, d->J, d->K);
     if (!isfinite(d->scaler)) return set_error(DM_ERR_ARG, "scaler=%g", d->scaler);
     // (the kernels' tanh is off by about 1e-7 of the cap)
     if (d->cap != 0.f && !(d->cap >= 0x1p-10f && d->cap <= 0x1p10f))
@@ -216,6 +237,9 @@ int attn_fwd(const dm_attn_desc* d, const void* q, const void* k, const void* v,
 int attn_bwd(const dm_attn_desc* d, const void* q, const void* k, const void* v, const void* out, const void* saved,
              const void* dout, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes, void* stream) {
     DM_TRY(check_desc(d));
+    if (!backward_fits(*d))
+        return set_error(DM_ERR_UNSUPPORTED, "B=%d H=%d G=%d J=%d K=%d: more blocks than a launch holds", d->B, d->H, d->G,
+                         d->J, d->K);
     DM_TRY(check_written(d->q, d->B, d->H, d->J, d->P, "dq"));
     DM_TRY(check_written(d->k, d->B, d->G, d->K, d->P, "dk"));
     DM_TRY(check_written(d->v, d->B, d->G, d->K, d->P, "dv"));
