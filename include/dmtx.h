@@ -371,7 +371,7 @@ typedef struct {
     const float* grad;       /* [n]                                            */
     void *m, *v;             /* [n], float or codes                            */
     float *m_scale, *v_scale;/* [(n + 255) / 256]; NULL for states in 32 bits  */
-    int64_t n;               /* 0: the tensor is left out                      */
+    int64_t n;               /* 0: the tensor is left out; up to 2^36 - 4096   */
     double decay;            /* weight decay, >= 0                             */
 } dm_adamw_tensor;
 

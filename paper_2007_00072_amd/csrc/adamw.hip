@@ -9,6 +9,8 @@ namespace {
 constexpr int NT = 256;
 constexpr int STATE_BLOCK = 256;   // elements of an 8-bit state that share a scale: 4 of each lane of a wave
 constexpr int CHUNK = 4096;        // elements of a block
+// blocks of a launch: a grid holds less than 2^32 threads along x (more wrap, without an error)
+constexpr int64_t BLOCKS = (((int64_t)1 << 32) - 1) / NT;
 constexpr float E4M3_MAX = 448.f;  // largest e4m3 value
 // blocks whose largest value is below 2^-100 are zeros (its reciprocal times 448 would overflow)
 constexpr float LEAST = 0x1p-100f;
@@ -184,7 +186,9 @@ void launch(const Job& j, int dtype, bool master, int bits, unsigned blocks, hip
 }
 
 int check_item(const dm_adamw_tensor& t, int i, const dm_adamw_desc& a) {
-    if (t.n < 0 || t.n > ((int64_t)1 << 42)) return set_error(DM_ERR_ARG, "tensor %d: n=%lld", i, (long long)t.n);
+    if (t.n < 0) return set_error(DM_ERR_ARG, "tensor %d: n=%lld", i, (long long)t.n);
+    if (t.n > BLOCKS * CHUNK)
+        return set_error(DM_ERR_UNSUPPORTED, "tensor %d: n=%lld is more than a launch holds", i, (long long)t.n);
     if (!(t.decay >= 0.) || !isfinite(t.decay)) return set_error(DM_ERR_ARG, "tensor %d: decay=%g", i, t.decay);
     if (t.n == 0) return DM_OK;
     const void* p[4] = {t.param, t.grad, t.m, t.v};
@@ -251,7 +255,7 @@ int adamw_step(const dm_adamw_desc* a, const dm_adamw_tensor* tensors, int32_t c
     uint32_t blocks = 0;
     for (int i = 0; i <= count; ++i) {
         const int64_t nb = i < count ? (tensors[i].n + CHUNK - 1) / CHUNK : 0;
-        if (j.n > 0 && (i == count || j.n == ITEMS || blocks + nb > INT32_MAX)) {
+        if (j.n > 0 && (i == count || j.n == ITEMS || blocks + nb > BLOCKS)) {
             launch(j, a->dtype, master, a->state_bits, blocks, st);
             j.n = 0;
             blocks = 0;

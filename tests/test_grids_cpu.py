@@ -36,3 +36,12 @@ def test_attention_backward_blocks(P, K, ok):
     with pytest.raises(lib.DmError) as e:
         lib.attn_bwd(d, *[PTR] * 9, PTR, bwd - 1, stream=0)
     assert e.value.code == (lib.DM_ERR_WORKSPACE if ok else lib.DM_ERR_UNSUPPORTED)
+
+
+@pytest.mark.parametrize("n", [2 ** 36 - 4095, 2 ** 42, 2 ** 63 - 1])
+def test_optimizer_blocks(n):
+    a = lib.AdamwDesc(lib.DM_BF16, 8, 1e-3, 0.9, 0.999, 1e-8, 1.0, 1, None)
+    t = (lib.AdamwTensor * 1)(lib.AdamwTensor(PTR, None, PTR, PTR, PTR, PTR, PTR, n, 0.0))
+    with pytest.raises(lib.DmError) as e:
+        lib.adamw_step(a, t, 1, stream=0)
+    assert e.value.code == lib.DM_ERR_UNSUPPORTED and "n=" in str(e.value)
