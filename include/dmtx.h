@@ -378,7 +378,7 @@ typedef struct {
 typedef struct {
     int32_t dtype;           /* dm_dtype of param                              */
     int32_t state_bits;      /* 32 or 8                                        */
-    double lr, beta1, beta2, eps;
+    double lr, beta1, beta2, eps;  /* eps: at least float32's smallest normal number */
     double grad_scale;       /* 1: gradients as they are                       */
     int64_t step;            /* 1 for the first                                */
     const float* scalars;    /* NULL, or device float[4] (16-byte aligned): lr,*/

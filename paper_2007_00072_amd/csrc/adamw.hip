@@ -1,4 +1,5 @@
 // AdamW (decoupled weight decay) over many tensors in few launches.
+#include <float.h>
 #include <math.h>
 
 #include "checks.hpp"
@@ -185,11 +186,15 @@ void launch(const Job& j, int dtype, bool master, int bits, unsigned blocks, hip
     else master ? launch<bf16_t, true>(j, bits, blocks, st) : launch<bf16_t, false>(j, bits, blocks, st);
 }
 
+// The step computes in float32: a number that is none there would make every
+// weight infinite or NaN.
+bool finite32(double x) { return isfinite((float)x); }
+
 int check_item(const dm_adamw_tensor& t, int i, const dm_adamw_desc& a) {
     if (t.n < 0) return set_error(DM_ERR_ARG, "tensor %d: n=%lld", i, (long long)t.n);
     if (t.n > BLOCKS * CHUNK)
         return set_error(DM_ERR_UNSUPPORTED, "tensor %d: n=%lld is more than a launch holds", i, (long long)t.n);
-    if (!(t.decay >= 0.) || !isfinite(t.decay)) return set_error(DM_ERR_ARG, "tensor %d: decay=%g", i, t.decay);
+    if (!(t.decay >= 0.) || !finite32(t.decay)) return set_error(DM_ERR_ARG, "tensor %d: decay=%g", i, t.decay);
     if (t.n == 0) return DM_OK;
     const void* p[4] = {t.param, t.grad, t.m, t.v};
     const char* n[4] = {"param", "grad", "m", "v"};
@@ -221,10 +226,12 @@ int adamw_step(const dm_adamw_desc* a, const dm_adamw_tensor* tensors, int32_t c
         return set_error(DM_ERR_UNSUPPORTED, "states in %d bits: 8 or 32", a->state_bits);
     if (!(a->beta1 >= 0. && a->beta1 < 1.) || !(a->beta2 >= 0. && a->beta2 < 1.))
         return set_error(DM_ERR_ARG, "beta1=%g beta2=%g outside [0,1)", a->beta1, a->beta2);
-    if (!(a->eps > 0.) || !isfinite(a->eps)) return set_error(DM_ERR_ARG, "eps must be > 0");
+    // (an eps that float32 holds as zero makes 0 / 0 of an element without a gradient)
+    if (!((float)a->eps >= FLT_MIN) || !finite32(a->eps))
+        return set_error(DM_ERR_ARG, "eps=%g must be > 0, a normal float32 number", a->eps);
     if (!a->scalars) {
-        if (!isfinite(a->lr) || a->lr < 0.) return set_error(DM_ERR_ARG, "lr=%g", a->lr);
-        if (!isfinite(a->grad_scale)) return set_error(DM_ERR_ARG, "grad_scale=%g", a->grad_scale);
+        if (!finite32(a->lr) || a->lr < 0.) return set_error(DM_ERR_ARG, "lr=%g", a->lr);
+        if (!finite32(a->grad_scale)) return set_error(DM_ERR_ARG, "grad_scale=%g", a->grad_scale);
         if (a->step < 1) return set_error(DM_ERR_ARG, "step=%lld: the first step is 1", (long long)a->step);
     } else {
         DM_TRY(check_ptr(a->scalars, "scalars"));
