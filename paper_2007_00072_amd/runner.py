@@ -110,9 +110,10 @@ def _dense(name, t, dtype, shape, device):
 
 def _launch(device, entry, *args):
     """An entry point on the device's current stream (and with the device as
-    the current one, where it is not already)."""
+    the current one, where it is not already).  The library takes device
+    pointers: host memory would be a fault of the kernels that read it."""
     if device.type != "cuda":
-        return entry(*args)
+        raise ValueError(f"tensors on {device}: the kernels run on a GPU's")
     if device.index == torch.cuda.current_device():
         return entry(*args, stream=torch.cuda.current_stream().cuda_stream)
     with torch.cuda.device(device):
