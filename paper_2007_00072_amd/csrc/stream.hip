@@ -82,8 +82,8 @@ bool backward_fits(const dm_attn_desc& d) {
 struct Sizes {
     size_t lo, saved;                     // saved: lse, then lo
     size_t ranges, part_o, part_ml, fwd;  // forward workspace: ends of its parts
-    size_t dsum, dmax, bwd;               // backward workspace (ranges first)
-    int splits, dmax_n, hparts;
+    size_t dsum, dmax, vmax, bwd;         // backward workspace (ranges first)
+    int splits, dmax_n, vmax_n, hparts;
 };
 
 Sizes sizes_of(const dm_attn_desc& d) {
@@ -100,8 +100,10 @@ Sizes sizes_of(const dm_attn_desc& d) {
     s.dmax_n = (d.J + STREAM_DROWS - 1) / STREAM_DROWS;
     s.dsum = s.ranges + align256(rows * 4);
     s.dmax = s.dsum + (d.dtype == DM_F16 ? align256((size_t)d.B * d.H * s.dmax_n * 4) : 0);
+    s.vmax_n = (d.K + stream_vmax_rows(d.K) - 1) / stream_vmax_rows(d.K);
+    s.vmax = s.dmax + (d.dtype == DM_F16 ? align256((size_t)d.B * d.G * s.vmax_n * 4) : 0);
     s.hparts = head_parts(d);
-    s.bwd = s.dmax + (s.hparts > 1 ? align256((size_t)s.hparts * d.B * d.G * d.K * 2 * d.P * 4) : 0);
+    s.bwd = s.vmax + (s.hparts > 1 ? align256((size_t)s.hparts * d.B * d.G * d.K * 2 * d.P * 4) : 0);
     return s;
 }
 
@@ -266,8 +268,11 @@ int attn_bwd(const dm_attn_desc* d, const void* q, const void* k, const void* v,
     a.dsum = (float*)((char*)ws + s.ranges);
     a.dmax = d->dtype == DM_F16 ? (float*)((char*)ws + s.dsum) : nullptr;
     a.dmax_n = s.dmax_n;
+    a.vmax = d->dtype == DM_F16 ? (float*)((char*)ws + s.dmax) : nullptr;
+    a.vmax_n = s.vmax_n;
+    a.vmax_rows = stream_vmax_rows(d->K);
     a.hparts = s.hparts;
-    a.part_k = (float*)((char*)ws + s.dmax);
+    a.part_k = (float*)((char*)ws + s.vmax);
     const hipStream_t st = S(stream);
     if (d->dtype == DM_F16) stream_bwd<half_t>(a, st);
     else if (d->dtype == DM_BF16) stream_bwd<bf16_t>(a, st);

@@ -2,6 +2,8 @@
 // instantiated per storage type, and the host code that launches them share.
 #pragma once
 
+#include <algorithm>
+
 #include "internal.hpp"
 
 namespace dm {
@@ -30,12 +32,16 @@ struct StreamArgs {
     float* dsum;     // backward: [B][H][J] row terms dout . out
     float* dmax;     // backward, fp16: [B][H][dmax_n] largest |dout| of row groups
     int dmax_n;
+    float* vmax;     // backward, fp16: [B][G][vmax_n] largest |v| of vmax_rows keys
+    int vmax_n, vmax_rows;
     int hparts;      // backward: parts the query heads of a key/value head are split into
     float* part_k;   // hparts > 1: [hparts][B][G][K][dk, dv]
 };
 
 constexpr int STREAM_RANGE = 64;   // keys of one entry of `ranges`
 constexpr int STREAM_DROWS = 256;  // rows of one entry of `dmax`
+// keys of one entry of `vmax`: so many that a wave reads all of a head's in four loads
+inline int stream_vmax_rows(int K) { return 256 * std::max(1, (K + 65535) / 65536); }
 
 // Row tiles and head sizes of the kernels (one function each for the host's
 // grid and the kernels' own constants).

@@ -731,20 +731,47 @@ __global__ __launch_bounds__(NT) void join_k(StreamArgs g) {
 // Row terms D = dout . out, out as the forward had it before rounding (its
 // stored value and the saved rest): LPR lanes a row, 8 elements each, four
 // rows of a lane group requested together.  fp16 also: the largest |dout| of
-// every 256 rows of a head, from which the score gradients get a power of
-// two that keeps them out of the type's subnormal numbers (a probability of
-// 1e-5 times a small gradient would lose its bits there).
+// every 256 rows of a head, and the largest |v| of vmax_rows keys of a
+// key/value head (blocks behind the rows'), from which the score gradients get
+// a power of two that keeps them inside the type (Gain).
 // Bound by reading three tensors: 262144 rows of 64 in bf16, 101 MB, in 20 us.
+__device__ __forceinline__ void block_max(float top, float* to) {
+    __shared__ float w[NT / 64];
+    top = group_max<64>(top);
+    if ((threadIdx.x & 63) == 0) w[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) *to = fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
+}
 template <typename T, int LPR>
 __global__ __launch_bounds__(NT) void rows_k(StreamArgs g) {
     constexpr int RPB = NT / LPR, U = 4;
-    const int nch = (g.J + STREAM_DROWS - 1) / STREAM_DROWS, z = (int)blockIdx.x / nch, ch = (int)blockIdx.x - z * nch;
-    const int b = z / g.H, h = z - b * g.H, gl = threadIdx.x % LPR, e = min(8 * gl, g.P - 8);
+    const int gl = threadIdx.x % LPR, e = min(8 * gl, g.P - 8);
+    const int nch = (g.J + STREAM_DROWS - 1) / STREAM_DROWS, nrows = nch * g.B * g.H;
+    float top = 0.f;
+    if (__is_same(T, half_t) && (int)blockIdx.x >= nrows) {
+        const int i = (int)blockIdx.x - nrows, z = i / g.vmax_n, k0 = (i - z * g.vmax_n) * g.vmax_rows;
+        const int b = z / g.G, end = min(k0 + g.vmax_rows, Seq(g, b).k_len);
+        const T* vp = reinterpret_cast<const T*>(g.v.ptr) + b * g.v.sb + (z - b * g.G) * g.v.sh + e;
+        for (int r0 = k0; r0 < end; r0 += RPB * U) {
+            float x[U][8];
+#pragma unroll
+            for (int u = 0; u < U; ++u) V8<T>::load(vp + (int64_t)min(r0 + u * RPB + (int)threadIdx.x / LPR, end - 1) * g.v.st, x[u]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int key = min(r0 + u * RPB + (int)threadIdx.x / LPR, end - 1);
+                if (g.doc && g.doc[(int64_t)b * g.K + key] < 0) continue;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[u][j]));
+            }
+        }
+        block_max(top, g.vmax + i);
+        return;
+    }
+    const int z = (int)blockIdx.x / nch, ch = (int)blockIdx.x - z * nch, b = z / g.H, h = z - b * g.H;
     const Seq s(g, b);
     const T* dp = reinterpret_cast<const T*>(g.dout.ptr) + b * g.dout.sb + h * g.dout.sh + e;
     const T* op = reinterpret_cast<const T*>(g.o.ptr) + b * g.o.sb + h * g.o.sh + e;
     const T* lp = reinterpret_cast<const T*>(g.lo) + ((int64_t)b * g.J * g.H + h) * g.P + e;
-    float top = 0.f;
     for (int r0 = 0; r0 < STREAM_DROWS; r0 += RPB * U) {
         float a[U][8], y[U][8], lo[U][8];
         bool in[U];
@@ -769,20 +796,15 @@ __global__ __launch_bounds__(NT) void rows_k(StreamArgs g) {
             if (gl == 0 && row < g.J) g.dsum[(int64_t)z * g.J + row] = d;
         }
     }
-    if (g.dmax) {
-        __shared__ float w[NT / 64];
-        top = group_max<64>(top);
-        if ((threadIdx.x & 63) == 0) w[threadIdx.x >> 6] = top;
-        __syncthreads();
-        if (threadIdx.x == 0) g.dmax[(int64_t)z * g.dmax_n + ch] = fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
-    }
+    if (g.dmax) block_max(top, g.dmax + (int64_t)z * g.dmax_n + ch);
 }
 
 // fp16: probabilities are held as 2^10 p; score gradients as 2^e ds with
-// 2^e about 1 / (2 max |dout|) over the heads of a key/value head, so that
-// they are at most p sum |v| (65504, the type's largest value, only where
-// values of 512 agree over a head of 128: such are held to it) and keep all
-// their bits down to 6e-5.
+// 2^e about 1 / (2 max |dout|) over the heads of a key/value head: there ds =
+// p (dout . v - D) is at most P max |v| / 2 (p (1 - p) is at most 1/4, and
+// dout . v differs between keys by up to 2 P |dout| |v|), so it keeps all its
+// bits down to 6e-5, and stays below 2^15 while P max |v| is up to 2^16.  Above
+// that, e falls by as many powers of two.
 struct Gain {
     float p2;   // added to the exponents of the probabilities
     float pinv; // 1 / 2^p2
@@ -795,20 +817,19 @@ __device__ __forceinline__ Gain gain(const StreamArgs& g, int b, int kvh) {
     const float* p = g.dmax + ((int64_t)b * g.H + kvh * (g.H / g.G)) * g.dmax_n;
     float top = 0.f;
     for (int i = threadIdx.x & 63; i < n; i += 64) top = fmaxf(top, p[i]);
+    const float* pv = g.vmax + ((int64_t)b * g.G + kvh) * g.vmax_n;
+    float v = 0.f;
+    for (int i = threadIdx.x & 63; i < g.vmax_n; i += 64) v = fmaxf(v, pv[i]);
     top = group_max<64>(top);
-    const int e = top > 0.f && top < INFINITY ? -1 - ilogbf(top) : 0;
+    v = group_max<64>(v) * (float)g.P;
+    const int less = v > 0x1p16f && v < INFINITY ? ilogbf(v) - 15 : 0;
+    const int e = top > 0.f && top < INFINITY ? -1 - ilogbf(top) - less : 0;
     return Gain{10.f, 1.f / 1024.f, ldexpf(1.f, e - 10), ldexpf(1.f, -e)};
 }
 // p (dout . v - D), scaled
 template <typename T> __device__ __forceinline__ float score_grad(float p, float dpd, const Gain& gn) {
     if constexpr (__is_same(T, half_t)) return p * dpd * gn.ds;
     return p * dpd;
-}
-// fp16: conversions to the type that pass its largest value give that value
-// instead of an infinity (infinities and NaN stay): bit 23 of the mode
-// register, while score gradients are formed
-template <typename T> __device__ __forceinline__ void hold_overflow(bool on) {
-    if constexpr (__is_same(T, half_t)) __builtin_amdgcn_s_setreg((23 << 6) | 1, on ? 1 : 0);
 }
 
 // dK and dV of 128 keys (32 a wave) of one key/value head: walks the query
@@ -933,7 +954,6 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
     cd.init(tid, g.P, g.dout.st);
     const uint32_t base = lds_offset(steps);
     auto rows_of = [&](int buf) { return reinterpret_cast<float*>(steps + buf * STEP + 2 * TB); };
-    hold_overflow<T>(true);
     const int h_end = min(grp, (part + 1) * ((grp + g.hparts - 1) / g.hparts));
     for (int hg = part * ((grp + g.hparts - 1) / g.hparts); hg < h_end; ++hg) {
         const int h = kvh * grp + hg;
@@ -1061,7 +1081,6 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
             }
         }
     }
-    hold_overflow<T>(false);
     if constexpr (QH == 2) {
         copied();  // (K and V, where no step waited for them)
         __syncthreads();
@@ -1241,7 +1260,6 @@ __device__ __forceinline__ void dq_block(const StreamArgs& g, int block, char* l
         fetch(s, 0);
         put(0);
     }
-    hold_overflow<T>(true);
     for (int buf = 0; s < steps; buf ^= NB - 1) {
         copied();
         __syncthreads();
@@ -1328,7 +1346,6 @@ __device__ __forceinline__ void dq_block(const StreamArgs& g, int block, char* l
         }
     }
     if (j >= g.J) return;
-    hold_overflow<T>(false);
     T* dqp = reinterpret_cast<T*>(g.dq.ptr) + b * g.dq.sb + h * g.dq.sh + (int64_t)j * g.dq.st;
     const float f = g.scaler * sc.SLOPE * gn.dsinv;
 #pragma unroll
@@ -1432,7 +1449,8 @@ template <typename T> void stream_fwd(const StreamArgs& a, bool few, hipStream_t
 template <typename T> void stream_bwd(const StreamArgs& a, hipStream_t st) {
     if (a.doc && a.K > 0) stream::ranges_k<T><<<dim3((unsigned)stream_ranges_n(a)), 64, 0, st>>>(a);
     if (a.J > 0) {
-        const int64_t n = (int64_t)((a.J + STREAM_DROWS - 1) / STREAM_DROWS) * a.B * a.H;
+        int64_t n = (int64_t)((a.J + STREAM_DROWS - 1) / STREAM_DROWS) * a.B * a.H;
+        if constexpr (__is_same(T, half_t)) n += (int64_t)a.vmax_n * a.B * a.G;
         if (a.P <= 32) stream::rows_k<T, 4><<<dim3((unsigned)n), stream::NT, 0, st>>>(a);
         else if (a.P <= 64) stream::rows_k<T, 8><<<dim3((unsigned)n), stream::NT, 0, st>>>(a);
         else stream::rows_k<T, 16><<<dim3((unsigned)n), stream::NT, 0, st>>>(a);
