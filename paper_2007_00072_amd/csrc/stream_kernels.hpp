@@ -149,11 +149,11 @@ template <bool ONCE> __device__ __forceinline__ void copy16(uint32_t lds, uint32
     if constexpr (ONCE)
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(lds), "v"(voff),
                      "s"(rsrc)
-                     : "memory");
+                     : "memory", "m0");
     else
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff),
                      "s"(rsrc)
-                     : "memory");
+                     : "memory", "m0");
 }
 // (The builtin tells the compiler that its own loads have come as well: else
 // it waits for one from ahead of a loop, a row's q, in every step of the
