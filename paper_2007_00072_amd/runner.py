@@ -214,7 +214,9 @@ class Attention:
 
 class Embedding:
     """Embedding lookup and gradient (embed_fwd / embed_bwd): table [V, I],
-    ids int32 of any shape, y ids.shape + [I], fp32 gradient [V, I]."""
+    ids int32 of any shape, y ids.shape + [I], fp32 gradient [V, I].  The
+    gradients of one object share its workspace and `grad`, captured ones
+    too, so two of them must not overlap."""
 
     def __init__(self, table: torch.Tensor, scale: float = 1.0, pad_id: int = -1):
         if table.dim() != 2:
@@ -224,7 +226,8 @@ class Embedding:
         self.scale, self.pad_id = scale, pad_id
         self.grad = torch.empty(table.shape, dtype=torch.float32, device=table.device)
         self.ws = torch.empty(0, dtype=torch.uint8, device=table.device)
-        self._outgrown = []  # workspaces that a captured backward may still use
+        self._used_on, self._captured = set(), False  # streams that the workspace was used on; by a capture
+        self._outgrown = []  # workspaces that captured backwards still use
 
     def forward(self, ids: torch.Tensor, y: Optional[torch.Tensor] = None) -> torch.Tensor:
         V, I = self.table.shape
@@ -240,13 +243,27 @@ class Embedding:
         V, I = self.table.shape
         _dense("ids", ids, torch.int32, ids.shape, self.device)
         _dense("dy", dy, self.table.dtype, (*ids.shape, I), self.device)
-        need = lib.embed_ws_bytes(ids.numel(), V, I)
-        if self.ws.numel() < need:
-            self._outgrown.append(self.ws)
-            self.ws = torch.empty(max(need, 2 * self.ws.numel()), dtype=torch.uint8, device=self.device)
+        self._make_room(lib.embed_ws_bytes(ids.numel(), V, I))
         _launch(self.device, lib.embed_bwd, self.code, ids.numel(), V, I, ids, self.pad_id, dy, self.scale,
                 self.grad, self.ws, self.ws.numel())
         return self.grad
+
+    def _make_room(self, need: int) -> None:
+        """A workspace of at least `need` bytes.  One that is outgrown stays
+        where a captured backward uses it; else its memory is free again once
+        the streams it was used on have come so far."""
+        if self.device.type != "cuda":
+            return
+        if self.ws.numel() < need:
+            if self._captured:
+                self._outgrown.append(self.ws)
+            else:
+                for s in self._used_on:
+                    self.ws.record_stream(s)
+            self.ws = torch.empty(max(need, 2 * self.ws.numel()), dtype=torch.uint8, device=self.device)
+            self._used_on, self._captured = set(), False
+        self._used_on.add(torch.cuda.current_stream(self.device))
+        self._captured |= torch.cuda.is_current_stream_capturing()
 
 
 STATE_BLOCK = 256  # elements of an 8-bit state that share a scale
