@@ -348,7 +348,9 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void fwd_k(StreamArgs g
     constexpr bool OWN = WK > 1;  // tiles of a wave's own
     using TL = Tile<T, DP>;
     constexpr int TB = BN * TL::PITCH;  // bytes of a step's keys
-    constexpr int NB = 4 * TB <= (OWN ? 65536 : 131072) ? 2 : 1;
+    // pairs of tiles: one is filled while the other is read (a wave's own: where two blocks then fit a CU)
+    constexpr int NB = !OWN || 4 * TB <= 65536 ? 2 : 1;
+    static_assert(OWN || 4 * TB <= 131072, "two pairs of tiles");
     constexpr int ROWS = OWN ? 32 * NS : BN, RB = ROWS * TL::PITCH;  // of a tile
     // joining the waves along the keys: m, l and o of all but the first
     constexpr int JOIN = WK > 1 ? (WK - 1) * 64 * (2 + 16 * ND) * 4 : 0;
@@ -498,7 +500,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void fwd_k(StreamArgs g
         if (!OWN || NB == 1) {
             nxt = next(cur + 1);
             nxt_mixed = mixed(nxt);
-            if (!OWN && NB == 2 && nxt < s_end) fetch(nxt, buf ^ 1);
+            if (!OWN && nxt < s_end) fetch(nxt, buf ^ 1);
         }
 
         floatx16 a[NS];
@@ -601,12 +603,8 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void fwd_k(StreamArgs g
                 then_mixed = mixed(then);
             }
             if (then < s_end && (NB == 1 || then != nxt)) fetch(then, NB == 2 ? buf : 0);
-        } else if (NB == 2) {
-            put(buf ^ 1);
         } else {
-            __syncthreads();
-            if (nxt < s_end) fetch(nxt, 0);
-            put(0);
+            put(buf ^ 1);
         }
         cur = nxt;
         cur_mixed = nxt_mixed;
@@ -849,8 +847,8 @@ template <typename T, int DP, int QH> struct DkvTiles {
     static constexpr int KT = QH == 2 ? STREAM_KEYS * Tile<T, DP>::PITCH : 0;  // of K, and of V
     // tiles of q and dout, and the rows' numbers: -lse, -D, bounds, documents
     static constexpr int STEP = 2 * TB + BQ * 16;
-    static constexpr int NB = 2 * STEP <= 131072 + 4096 ? 2 : 1;
-    static constexpr int LDS = 2 * KT + NB * STEP;
+    static constexpr int LDS = 2 * KT + 2 * STEP;  // one step's tiles are filled while the other's are read
+    static_assert(LDS <= 160 * 1024, "LDS of a CU");
 };
 template <typename T, int DP, bool CAP, bool BIAS, int QH>
 __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* lds) {
@@ -858,7 +856,7 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
     constexpr bool FRAGS = sizeof(T) == 2 && QH == 1;
     using TL = Tile<T, DP>;
     using Tiles = DkvTiles<T, DP, QH>;
-    constexpr int TB = Tiles::TB, STEP = Tiles::STEP, NB = Tiles::NB;
+    constexpr int TB = Tiles::TB, STEP = Tiles::STEP;
     int tile, z;
     place(block, g.B * g.G * g.hparts, tile, z);
     const int part = z % g.hparts;
@@ -994,7 +992,7 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
             fetch(s, 0);
             put(0);
         }
-        for (int buf = 0; s < nst; buf ^= NB - 1) {
+        for (int buf = 0; s < nst; buf ^= 1) {
             copied();
             __syncthreads();
             const int j0 = s * BQ;
@@ -1003,7 +1001,7 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
             const char *tq = steps + buf * STEP, *td = tq + TB;
             const float* rows = rows_of(buf);
             s = next(s + 1);
-            if (NB == 2 && s < nst) fetch(s, buf ^ 1);
+            if (s < nst) fetch(s, buf ^ 1);
 #pragma unroll
             for (int n0 = 0; n0 < BQ / 32; n0 += QH) {
                 const int n = QH == 2 ? qh : n0;
@@ -1072,13 +1070,7 @@ __device__ __forceinline__ void dkv_block(const StreamArgs& g, int block, char* 
                     }
                 }
             }
-            if (NB == 2) {
-                put(buf ^ 1);
-            } else {
-                __syncthreads();
-                if (s < nst) fetch(s, 0);
-                put(0);
-            }
+            put(buf ^ 1);
         }
     }
     if constexpr (QH == 2) {
@@ -1157,16 +1149,17 @@ __global__ __launch_bounds__(NT) void dkv_join_k(StreamArgs g) {
 // and adding nothing atomically.  8192 causal tokens, capped, 16 heads of
 // 128: 575 us, 0.72 PFLOP/s.
 template <typename T, int DP> struct DqTiles {
-    static constexpr int BN = 64, TB = BN * Tile<T, DP>::PITCH, NB = 4 * TB <= 131072 ? 2 : 1;
-    static constexpr int LDS = 2 * NB * TB + 2 * BN * 4 + 4 * 8;  // tiles, documents of the keys, of the waves' rows
+    static constexpr int BN = 64, TB = BN * Tile<T, DP>::PITCH;
+    static constexpr int LDS = 4 * TB + 2 * BN * 4 + 4 * 8;  // two pairs of tiles, documents of the keys, of the waves' rows
+    static_assert(LDS <= 160 * 1024, "LDS of a CU");
 };
 template <typename T, int DP, bool CAP, bool BIAS>
 __device__ __forceinline__ void dq_block(const StreamArgs& g, int block, char* lds) {
     constexpr int BM = 128, BN = 64, NS = 2, ND = DP / 32, NC = DP / 16;
     using TL = Tile<T, DP>;
     using Tiles = DqTiles<T, DP>;
-    constexpr int TB = Tiles::TB, NB = Tiles::NB;
-    int* kdoc = reinterpret_cast<int*>(lds + 2 * NB * TB);
+    constexpr int TB = Tiles::TB;
+    int* kdoc = reinterpret_cast<int*>(lds + 4 * TB);
     int2* wrange = reinterpret_cast<int2*>(kdoc + 2 * BN);
     const int nqt = (g.J + BM - 1) / BM;
     int tile, z;
@@ -1260,14 +1253,14 @@ __device__ __forceinline__ void dq_block(const StreamArgs& g, int block, char* l
         fetch(s, 0);
         put(0);
     }
-    for (int buf = 0; s < steps; buf ^= NB - 1) {
+    for (int buf = 0; s < steps; buf ^= 1) {
         copied();
         __syncthreads();
         const int k0 = s * BN;
         const char *tk = lds + buf * 2 * TB, *tv = tk + TB;
         const bool mixed = docs && !win.is(win.whole, s);
         s = next(s + 1);
-        if (NB == 2 && s < steps) fetch(s, buf ^ 1);
+        if (s < steps) fetch(s, buf ^ 1);
 #pragma unroll 1
         for (int n = 0; n < NS; ++n) {
             floatx16 x, dpd;
@@ -1337,13 +1330,7 @@ __device__ __forceinline__ void dq_block(const StreamArgs& g, int block, char* l
                     dq[d] = mma<T>(COLS ? cf[c][COLS ? d : 0] : TL::col(tk, 32 * n + 16 * c, 32 * d, lane), sf, dq[d]);
             }
         }
-        if (NB == 2) {
-            put(buf ^ 1);
-        } else {
-            __syncthreads();
-            if (s < steps) fetch(s, 0);
-            put(0);
-        }
+        put(buf ^ 1);
     }
     if (j >= g.J) return;
     T* dqp = reinterpret_cast<T*>(g.dq.ptr) + b * g.dq.sb + h * g.dq.sh + (int64_t)j * g.dq.st;
