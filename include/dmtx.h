@@ -424,6 +424,15 @@ int saved_tensor_view(const dm_layer_desc* d, int32_t id, size_t* offset, size_t
  * storage type, row term sum_k dP P).  The two differ only in rounding. */
 int attn_backward_form(const dm_layer_desc* d, int32_t* key_blocks);
 
+/* Which forms attn_fwd and attn_bwd take with this descriptor (its sizes
+ * decide): *rows = query rows of a forward block (128, or 32 whose waves walk
+ * keys of their own), *key_parts = parts the forward's keys are split into,
+ * *head_parts = parts of a key/value head's query heads in the backward,
+ * *apart = 1 where the backward's two halves are launches of their own.  Any
+ * may be NULL.  The forms differ only in rounding. */
+int attn_form(const dm_attn_desc* d, int32_t* rows, int32_t* key_parts, int32_t* head_parts,
+              int32_t* apart);
+
 /* General contraction on the library's MFMA kernel, for op-level tests:
  * C[z][m][n] = alpha * sum_k A[z][m][k] * B[z][k][n] (+ bias[n]) with
  * row-major operands, `a_trans` / `b_trans` selecting A stored [K][M] /

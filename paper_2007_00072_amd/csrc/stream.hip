@@ -63,20 +63,25 @@ int head_parts(const dm_attn_desc& d) {
 // A grid holds less than 2^32 threads along x (more wrap, without an error).
 constexpr int64_t GRID_THREADS = ((int64_t)1 << 32) - 1;
 
+int64_t forward_blocks(const dm_attn_desc& d) {
+    const int64_t bm = few_rows(d) ? STREAM_BM_FEW : STREAM_BM, pack = packed_heads(d);
+    return ((int64_t)d.J * pack + bm - 1) / bm * d.B * (d.H / pack) * key_splits(d);
+}
+int64_t key_blocks(const dm_attn_desc& d) {
+    return ((int64_t)d.K + STREAM_KEYS - 1) / STREAM_KEYS * d.B * d.G * head_parts(d);
+}
+int64_t row_blocks(const dm_attn_desc& d) { return ((int64_t)d.J + STREAM_BM - 1) / STREAM_BM * d.B * d.H; }
+
 // Threads of the forward's launches: row tiles, ranges of documents.  (The
 // parts are joined only where there are few rows.)
 bool forward_fits(const dm_attn_desc& d) {
-    const int64_t bm = few_rows(d) ? STREAM_BM_FEW : STREAM_BM, pack = packed_heads(d);
-    const int64_t blocks = ((int64_t)d.J * pack + bm - 1) / bm * d.B * (d.H / pack) * key_splits(d);
     const int64_t ranges = d.doc ? ((int64_t)d.K + STREAM_RANGE - 1) / STREAM_RANGE * d.B : 0;
-    return blocks * 256 <= GRID_THREADS && ranges * 64 <= GRID_THREADS;
+    return forward_blocks(d) * 256 <= GRID_THREADS && ranges * 64 <= GRID_THREADS;
 }
 // Of the backward's: key tiles (wide heads: 512 threads each) and row tiles,
 // in one launch or two; the row terms' blocks are fewer than the row tiles.
 bool backward_fits(const dm_attn_desc& d) {
-    const int64_t keys = ((int64_t)d.K + STREAM_KEYS - 1) / STREAM_KEYS * d.B * d.G * head_parts(d);
-    const int64_t rows = ((int64_t)d.J + STREAM_BM - 1) / STREAM_BM * d.B * d.H;
-    return (keys * (d.P > 64 ? 2 : 1) + rows) * 256 <= GRID_THREADS;
+    return (key_blocks(d) * (d.P > 64 ? 2 : 1) + row_blocks(d)) * 256 <= GRID_THREADS;
 }
 
 struct Sizes {
@@ -200,6 +205,15 @@ int attn_sizes(const dm_attn_desc* d, size_t* saved_bytes, size_t* fwd_ws_bytes,
     if (saved_bytes) *saved_bytes = s.saved;
     if (fwd_ws_bytes) *fwd_ws_bytes = s.fwd;
     if (bwd_ws_bytes) *bwd_ws_bytes = s.bwd;
+    return DM_OK;
+}
+
+int attn_form(const dm_attn_desc* d, int32_t* rows, int32_t* key_parts, int32_t* head_parts_, int32_t* apart) {
+    DM_TRY(check_desc(d));
+    if (rows) *rows = few_rows(*d) ? STREAM_BM_FEW : STREAM_BM;
+    if (key_parts) *key_parts = key_splits(*d);
+    if (head_parts_) *head_parts_ = head_parts(*d);
+    if (apart) *apart = stream_apart(d->P, key_blocks(*d) + row_blocks(*d)) ? 1 : 0;
     return DM_OK;
 }
 

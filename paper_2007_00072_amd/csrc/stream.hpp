@@ -55,6 +55,7 @@ constexpr int STREAM_BN = 64, STREAM_BN_FEW = 128;  // keys of a step
 // causal queries in 16 heads of 128; 300 queries in 16 heads take 45 us in
 // one launch and 60 in two.  Up to 64 one launch is never slower.)
 constexpr int STREAM_BOTH = 512;
+constexpr bool stream_apart(int head, int64_t blocks) { return head > 64 && blocks > STREAM_BOTH; }
 constexpr int STREAM_KEYS = 128;                    // keys of a block of the dK / dV kernel
 
 template <typename T> void stream_fwd(const StreamArgs& a, bool few, hipStream_t st);

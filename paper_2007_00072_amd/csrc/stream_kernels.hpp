@@ -1385,7 +1385,7 @@ template <typename T, int DP, bool CAP, bool BIAS> void launch_bwd(const StreamA
     const int64_t nk = (int64_t)((a.K + STREAM_KEYS - 1) / STREAM_KEYS) * a.B * a.G;
     const int64_t nq = (int64_t)((a.J + 127) / 128) * a.B * a.H;
     const int64_t nkb = nk * a.hparts;
-    if (DP <= 64 || nkb + nq <= STREAM_BOTH) {
+    if (!stream_apart(DP, nkb + nq)) {
         dkv_dq_k<T, DP, CAP, BIAS><<<dim3((unsigned)(nkb + nq)), NT, 0, st>>>(a, (int)nkb);
     } else if constexpr (DP > 64) {
         constexpr int QH = sizeof(T) == 2 ? 2 : 1;  // (two tiles of float32 keys and rows do not fit LDS together)

@@ -47,7 +47,7 @@ EXPORTED = [
     "dropout_mask", "saved_tensor_view", "attn_backward_form", "contract", "dm_last_error",
     "dm_trace_enable", "dm_trace_count", "dm_trace_get",
     "plan_create", "plan_destroy", "plan_log", "plan_log_read",
-    "attn_sizes", "attn_fwd", "attn_bwd", "embed_ws_bytes", "embed_fwd", "embed_bwd", "adamw_step",
+    "attn_sizes", "attn_form", "attn_fwd", "attn_bwd", "embed_ws_bytes", "embed_fwd", "embed_bwd", "adamw_step",
 ]
 
 
@@ -173,6 +173,7 @@ _f["dm_trace_get"] = _sig("dm_trace_get", I32, I32, C.POINTER(C.c_char_p), C.POI
                           C.POINTER(C.c_float))
 PATTN = C.POINTER(AttnDesc)
 _f["attn_sizes"] = _sig("attn_sizes", I32, PATTN, PSZ, PSZ, PSZ)
+_f["attn_form"] = _sig("attn_form", I32, PATTN, C.POINTER(I32), C.POINTER(I32), C.POINTER(I32), C.POINTER(I32))
 _f["attn_fwd"] = _sig("attn_fwd", I32, PATTN, P_, P_, P_, P_, P_, P_, SZ, P_)
 _f["attn_bwd"] = _sig("attn_bwd", I32, PATTN, P_, P_, P_, P_, P_, P_, P_, P_, P_, P_, SZ, P_)
 _f["embed_ws_bytes"] = _sig("embed_ws_bytes", SZ, I64, I32, I32)
@@ -377,6 +378,13 @@ def attn_sizes(desc: AttnDesc):
     s, f, b = C.c_size_t(), C.c_size_t(), C.c_size_t()
     _call("attn_sizes", C.byref(desc), C.byref(s), C.byref(f), C.byref(b))
     return s.value, f.value, b.value
+
+
+def attn_form(desc: AttnDesc):
+    """(rows of a forward block, key parts, head parts of the backward, backward in two launches)."""
+    r, k, h, a = I32(), I32(), I32(), I32()
+    _call("attn_form", C.byref(desc), C.byref(r), C.byref(k), C.byref(h), C.byref(a))
+    return r.value, k.value, h.value, bool(a.value)
 
 
 def attn_fwd(desc: AttnDesc, q, k, v, out, saved, ws, ws_bytes, stream=None):
