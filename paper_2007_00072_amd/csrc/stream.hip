@@ -151,8 +151,10 @@ int check_desc(const dm_attn_desc* d) {
         return set_error(DM_ERR_ARG, "H=%d heads are no multiple of G=%d key/value heads", d->H, d->G);
     if (d->P <= 0 || d->P % 8 || d->P > 128)
         return set_error(DM_ERR_UNSUPPORTED, "head size P=%d is not a multiple of 8 up to 128", d->P);
-    if ((int64_t)d->B * d->H * d->J > INT32_MAX || (int64_t)d->B * d->G * d->K > INT32_MAX || d->J > (1 << 30) ||
-        d->K > (1 << 30) || (int64_t)d->H * d->J > INT32_MAX || (int64_t)d->B * d->H > INT32_MAX / 64)
+    // (products of three sizes are formed once those of two are known to be small)
+    if (d->J > (1 << 30) || d->K > (1 << 30) || (int64_t)d->B * d->H > INT32_MAX / 64 ||
+        (int64_t)d->H * d->J > INT32_MAX || (int64_t)d->B * d->H * d->J > INT32_MAX ||
+        (int64_t)d->B * d->G * d->K > INT32_MAX)
         return set_error(DM_ERR_UNSUPPORTED, "B=%d H=%d G=%d J=%d K=%d: more than 2^31 - 1 rows", d->B, d->H, d->G, d->J,
                          d->K);
     if (!forward_fits(*d))

@@ -24,6 +24,16 @@ def test_attention_blocks(B, J, K, H, G):
     assert e.value.code == lib.DM_ERR_UNSUPPORTED and "blocks" in str(e.value)
 
 
+@pytest.mark.parametrize("B,J,K,H,G", [(2 ** 31 - 1,) * 5, (2 ** 31 - 1, 2 ** 31 - 1, 1, 2 ** 30, 1),
+                                       (1, 1, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1)])
+def test_sizes_whose_products_pass_64_bits(B, J, K, H, G):
+    d = attn(1, 1, 1, 1, 1, 8)
+    d.B, d.J, d.K, d.H, d.G = B, J, K, H, G
+    with pytest.raises(lib.DmError) as e:
+        lib.attn_sizes(d)
+    assert e.value.code == lib.DM_ERR_UNSUPPORTED and "rows" in str(e.value)
+
+
 def test_attention_blocks_that_fit():
     for B, J, K, H, G in ((2 ** 21 - 1, 1, 1, 8, 8), (2 ** 24 - 1, 1, 1, 1, 1), (1, 2 ** 30, 1, 1, 1), (8, 512, 512, 16, 16)):
         lib.attn_sizes(attn(B, J, K, H, G, 8))
