@@ -110,14 +110,19 @@ def _dense(name, t, dtype, shape, device):
 
 def _launch(device, entry, *args):
     """An entry point on the device's current stream (and with the device as
-    the current one, where it is not already).  The library takes device
-    pointers: host memory would be a fault of the kernels that read it."""
+    the current one, where it is not already); the stream's handle.  The
+    library takes device pointers: host memory would be a fault of the kernels
+    that read it."""
     if device.type != "cuda":
         raise ValueError(f"tensors on {device}: the kernels run on a GPU's")
     if device.index == torch.cuda.current_device():
-        return entry(*args, stream=torch.cuda.current_stream().cuda_stream)
+        stream = torch.cuda.current_stream().cuda_stream
+        entry(*args, stream=stream)
+        return stream
     with torch.cuda.device(device):
-        return entry(*args, stream=torch.cuda.current_stream().cuda_stream)
+        stream = torch.cuda.current_stream().cuda_stream
+        entry(*args, stream=stream)
+    return stream
 
 
 def _code(dtype: torch.dtype) -> int:
@@ -226,7 +231,7 @@ class Embedding:
         self.scale, self.pad_id = scale, pad_id
         self.grad = torch.empty(table.shape, dtype=torch.float32, device=table.device)
         self.ws = torch.empty(0, dtype=torch.uint8, device=table.device)
-        self._used_on, self._captured = set(), False  # streams that the workspace was used on; by a capture
+        self._used_on, self._captured = set(), False  # streams that used the workspace; whether a capture may have
         self._outgrown = []  # workspaces that captured backwards still use
 
     def forward(self, ids: torch.Tensor, y: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -243,27 +248,28 @@ class Embedding:
         V, I = self.table.shape
         _dense("ids", ids, torch.int32, ids.shape, self.device)
         _dense("dy", dy, self.table.dtype, (*ids.shape, I), self.device)
-        self._make_room(lib.embed_ws_bytes(ids.numel(), V, I))
-        _launch(self.device, lib.embed_bwd, self.code, ids.numel(), V, I, ids, self.pad_id, dy, self.scale,
-                self.grad, self.ws, self.ws.numel())
+        need = lib.embed_ws_bytes(ids.numel(), V, I)
+        if self.ws.numel() < need:
+            self._grow(need)
+        stream = _launch(self.device, lib.embed_bwd, self.code, ids.numel(), V, I, ids, self.pad_id, dy, self.scale,
+                         self.grad, self.ws, self.ws.numel())
+        self._used_on.add(stream)
+        # (the question is about the current device's stream)
+        if torch.cuda.is_current_stream_capturing() or self.device.index != torch.cuda.current_device():
+            self._captured = True
         return self.grad
 
-    def _make_room(self, need: int) -> None:
-        """A workspace of at least `need` bytes.  One that is outgrown stays
-        where a captured backward uses it; else its memory is free again once
-        the streams it was used on have come so far."""
-        if self.device.type != "cuda":
-            return
-        if self.ws.numel() < need:
-            if self._captured:
-                self._outgrown.append(self.ws)
-            else:
-                for s in self._used_on:
-                    self.ws.record_stream(s)
-            self.ws = torch.empty(max(need, 2 * self.ws.numel()), dtype=torch.uint8, device=self.device)
-            self._used_on, self._captured = set(), False
-        self._used_on.add(torch.cuda.current_stream(self.device))
-        self._captured |= torch.cuda.is_current_stream_capturing()
+    def _grow(self, need: int) -> None:
+        """A larger workspace.  The one it replaces stays where a captured
+        backward uses it; else its memory is free again once the streams it
+        was used on have come so far."""
+        if self._captured:
+            self._outgrown.append(self.ws)
+        else:
+            for s in self._used_on:
+                self.ws.record_stream(torch.cuda.ExternalStream(s, self.device))
+        self.ws = torch.empty(max(need, 2 * self.ws.numel()), dtype=torch.uint8, device=self.device)
+        self._used_on, self._captured = set(), False
 
 
 STATE_BLOCK = 256  # elements of an 8-bit state that share a scale
