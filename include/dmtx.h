@@ -281,7 +281,7 @@ int residual_add(int32_t dtype, int64_t n, const void* a, const void* b, void* o
  * elements of q, k, v and dout have to be finite (a key that is hidden from
  * one query only by causal or by its document takes part as 0 times its
  * value).  Query head h reads key/value head h / (H / G).
- * Scores are float32 and, without a cap, stay within 2^26 in magnitude (else
+ * Scores are float32 and, without a cap, stay within 2^24 in magnitude (else
  * infinities and NaN may come out).  The backward forms probabilities from a
  * float32 log-sum of the scores: a score's magnitude times 2^-24 adds to their
  * relative error.

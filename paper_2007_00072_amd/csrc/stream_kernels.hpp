@@ -470,9 +470,15 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void fwd_k(StreamArgs g
     for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-    // m: in the scores' own units
+    // m: in the scores' own units.  What is summed is 2^UP p with p relative to
+    // 2^m: 2^10 in fp16, as in the backward, whose normal numbers then hold
+    // probabilities down to 2^-24 (many of 2^-22 behind one large one are what
+    // a long sequence sums up; they had one or two bits there), and the
+    // reference follows closer so that 2^14 is the largest.
+    constexpr bool HALF = __is_same(T, half_t);
+    constexpr float UP = HALF ? 10.f : 0.f;
     float m = -INFINITY, l = 0.f;
-    const float f = BIAS ? 1.f : sc.scale, slack = 8.f / f;
+    const float f = BIAS ? 1.f : sc.scale, slack = (HALF ? 4.f : 8.f) / f;
 
     auto mixed = [&](int step) { return docs && step < s_end && !win.is(win.whole, step); };
     int cur = next(split * per), nxt = s_end;
@@ -565,7 +571,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void fwd_k(StreamArgs g
         const Halves both = halves(mx);
         mx = fmaxf(both.lo, both.hi);
         // the row's reference value follows its maximum only once that is 2^8
-        // above it: until then sums and products stay far inside their types
+        // (fp16: 2^4) above it: until then sums and products stay inside their types
         if (__any(mx > m + slack)) {
             const float mn = fmaxf(m, mx);
             const float alpha = mn == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * f);
@@ -576,7 +582,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void fwd_k(StreamArgs g
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
         }
-        const float mf = m == -INFINITY ? 0.f : -m * f;
+        const float mf = m == -INFINITY ? 0.f : fmaf(-m, f, UP);
         float p[NS][16];
 #pragma unroll
         for (int n = 0; n < NS; ++n)
@@ -611,7 +617,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void fwd_k(StreamArgs g
         nxt = then;
         nxt_mixed = then_mixed;
     }
-    m = m * f + sc.offset;  // from here in units of log2
+    m = fmaf(m, f, sc.offset - UP);  // from here in units of log2
     if (hi == 0) {  // a row that sees nothing
         m = -INFINITY;
         l = 0.f;

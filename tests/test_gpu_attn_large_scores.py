@@ -23,7 +23,7 @@ def float32_by_default():
 @pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("J", [3, 300])
 @pytest.mark.parametrize("sign", [1, -1])
-@pytest.mark.parametrize("log", [10, 14, 18, 26])
+@pytest.mark.parametrize("log", [10, 14, 18, 24])
 def test_one_key_takes_all(dt, J, sign, log):
     # all products are exact; the largest score 2^log and the others half of it, or -2^(log - 1) and -2^log
     B, K, H, P, scaler = 2, 520, 8, 64, 0.125
