@@ -804,11 +804,11 @@ __global__ __launch_bounds__(NT) void rows_k(StreamArgs g) {
 }
 
 // fp16: probabilities are held as 2^10 p; score gradients as 2^e ds with
-// 2^e about 1 / (2 max |dout|) over the heads of a key/value head: there ds =
-// p (dout . v - D) is at most P max |v| / 2 (p (1 - p) is at most 1/4, and
-// dout . v differs between keys by up to 2 P |dout| |v|), so it keeps all its
-// bits down to 6e-5, and stays below 2^15 while P max |v| is up to 2^16.  Above
-// that, e falls by as many powers of two.
+// 2^e = 2^14 over the powers of two below max |dout| (of the heads of a
+// key/value head) and P max |v|.  ds = p (dout . v - D) is at most P max |dout|
+// max |v| / 2 (p (1 - p) is at most 1/4, and dout . v differs between keys by
+// up to 2 P |dout| |v|), so what is held stays below 2^15, the type's numbers
+// end at 2^16, and it keeps all its bits down to 2^-29 of that bound.
 struct Gain {
     float p2;   // added to the exponents of the probabilities
     float pinv; // 1 / 2^p2
@@ -826,8 +826,8 @@ __device__ __forceinline__ Gain gain(const StreamArgs& g, int b, int kvh) {
     for (int i = threadIdx.x & 63; i < g.vmax_n; i += 64) v = fmaxf(v, pv[i]);
     top = group_max<64>(top);
     v = group_max<64>(v) * (float)g.P;
-    const int less = v > 0x1p16f && v < INFINITY ? ilogbf(v) - 15 : 0;
-    const int e = top > 0.f && top < INFINITY ? -1 - ilogbf(top) - less : 0;
+    const bool known = top > 0.f && top < INFINITY && v > 0.f && v < INFINITY;  // (else all gradients of scores are zeros)
+    const int e = known ? 14 - ilogbf(top) - ilogbf(v) : 0;
     return Gain{10.f, 1.f / 1024.f, ldexpf(1.f, e - 10), ldexpf(1.f, -e)};
 }
 // p (dout . v - D), scaled

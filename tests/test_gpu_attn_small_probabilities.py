@@ -1,6 +1,6 @@
 """fp16 attention where one key has nearly all of the softmax and a value of
-zero (a sink), so that the output is a sum of many probabilities below fp16's
-normal numbers."""
+zero (a sink), so that outputs and gradients are sums over many probabilities
+below fp16's normal numbers."""
 import math
 
 import pytest
@@ -53,3 +53,33 @@ def test_a_sink_and_many_small_ones(dt, J, steps, sink):
     # in lanes, waves and parts (64 at the least of them, sums of up to K / 64 terms)
     room = 2.02 * U[dt] + 2.0 ** -20 + (K / 64 + 64) * 2.0 ** -24
     assert ((out - want).abs() <= room * want).all(), float(((out - want).abs() / want).max())
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("J", [1, 200])
+@pytest.mark.parametrize("P", [32, 128])
+@pytest.mark.parametrize("steps", [2, 9])
+def test_gradients_of_a_row_with_small_ones(dt, J, P, steps):
+    # one element of dout is 64 times the others, and no value answers to it
+    K, H = 8192, 2
+    s = worst_score(steps, dt)
+    q, k, v, dout = torch.zeros(1, J, H, P), torch.zeros(1, K, H, P), torch.zeros(1, K, H, P), torch.zeros(1, J, H, P)
+    q[..., 0] = 1.0
+    k[:, 1:, :, 0] = s
+    v[:, 1:, :, 1:] = 0.75
+    dout[...] = 2.0 ** -6
+    dout[..., 0] = 1.0
+    d = [t.to(T[dt]).to(DEV) for t in (q, k, v)]
+    a = runner.Attention(*d, scaler=1.0)
+    out = a.forward(*d)
+    dq, _, _ = a.backward(*d, out, dout.to(T[dt]).to(DEV))
+    p, c = math.exp(s), (P - 1) * 0.75 * 2.0 ** -6
+    one, rest = p / (1 + (K - 1) * p), (K - 1) * p / (1 + (K - 1) * p)
+    want = rest * (1 - rest) * c * s
+    # a score's gradient is held times 2^e: |dout| 2^e is 2^-1 for the largest, times 2^15 over the power of two below
+    # P |v|; half of fp16's smallest number of that
+    held = one * c * (1 - rest) * 2.0 ** (14 - math.floor(math.log2(P * 0.75)))
+    room = (2.0 ** -25 / held if dt == "f16" else 0.0) + 3.1 * U[dt] + 2.0 ** -14 + K / 2 * 2.0 ** -24
+    got = dq[..., 0].cpu().double()
+    assert ((got - want).abs() <= room * abs(want)).all(), (float(got[0, 0, 0]), want, room)
+    assert not dq[..., 1:].any()
