@@ -106,7 +106,7 @@ template <bool ROOT> __device__ __forceinline__ float pack4(uint8_t* p, int n, c
 
 // One pass over everything, 4 elements a lane at a time.  Bound by memory: 12.6
 // million fp16 weights with fp32 copies and states (30 bytes each, 378 MB) in
-// 70 us, 5.4 TB/s; 302 million bf16 weights with fp32 copies and 8-bit states
+// 76 us, 5.0 TB/s; 302 million bf16 weights with fp32 copies and 8-bit states
 // (18 bytes each) in 1090, 5.0.  16 tensors of 32 to 4096: 6.5 us, a launch.
 template <typename T, bool MASTER, int BITS>
 __global__ __launch_bounds__(NT) void adamw_k(Job job) {

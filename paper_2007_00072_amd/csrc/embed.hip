@@ -18,7 +18,7 @@ __device__ __forceinline__ int64_t block_of_rows() { return (int64_t)blockIdx.y 
 
 // y[t] = scale table[ids[t]]: `lanes` lanes a token (a power of two), 16
 // bytes of the storage type each at a time.  Bound by memory: 16384 tokens of
-// 1024 in fp16, 34 MB read and 34 written, in 13.5 us.
+// 1024 in fp16, 34 MB read and 34 written, in 12.7 us.
 template <typename T>
 __global__ __launch_bounds__(NT) void embed_fwd_k(int64_t tokens, int vocab, int cols, int lanes, const int32_t* ids,
                                                   const T* table, float scale, T* y) {
@@ -43,21 +43,30 @@ __global__ __launch_bounds__(NT) void embed_fwd_k(int64_t tokens, int vocab, int
 // (stable: the order of the sums is given by the ids alone), then every
 // wave adds up a piece of the sorted list, writing the rows whose tokens all
 // lie there and leaving partial sums of the first and the last otherwise,
-// which a last pass joins in order.  So the work is even however often an id
-// occurs, dy is read once, and rows that no token has come from the fill
-// that runs beside the sort: the pass is bound by writing dtable and reading
-// dy.
+// which a last pass joins in order.  dy is read once, evenly, and rows that no
+// token has come from the fill that runs beside the sort: the pass is bound by
+// writing dtable and reading dy, while no id has a large share of the tokens.
+// An id's parts are joined by one wave (for each 256 columns): 16384 tokens of
+// 1024 in fp16 take 51 us as words are and 101 with two ids, 131072 with two
+// ids 790.
 //
 // The sort: up to 16384 tokens in lists of 1024, each by one block in LDS
 // while the other blocks of the launch fill; a second launch places every
 // token by counting, in each list, what comes before it.  (One block for all
 // 16384 takes 52 us: the ballots of a radix pass are bound by its CU's
-// vector units.)  More tokens by passes over blocks of tokens (count, scan,
-// place).
+// vector units.)  16384 is what 14 bits of a token's number beside 18 of its id
+// and 64 KB of LDS for all lists hold.  More tokens, or ids past 18 bits, by
+// passes over blocks of tokens (count, scan, place: three launches for each 8
+// bits of the ids, with 4096 tokens or more a block): 16385 tokens of 1024 in
+// fp16 101 us, 65536 173, 2^20 1500 (1060 with ids evenly spread).
 constexpr int PIECE = 8;           // sorted tokens of a wave, all requested together
 constexpr int PIECE_FEW = 4;       // up to RUN_TOKENS tokens: shorter chains
-constexpr int RUN_TOKENS = 1024;   // up to here a wave follows its last id to the end instead of leaving it in parts:
-                                   // one launch less where launches are what counts
+// Up to RUN_TOKENS a wave follows its last id to the end instead of leaving it
+// in parts: one launch less.  768 columns in bf16, ids as words are: 256 tokens
+// 19 us, 512 21, 1024 29, where 1025 in parts take 30.  A wave adds a long run
+// by itself, four tokens at a time: tokens all of one id take 49 us for 128, 145
+// for 512 and 270 for 1024, 34 for 1025 in parts.
+constexpr int RUN_TOKENS = 1024;
 constexpr int SORT_TOKENS = 16384;
 constexpr int IDX_BITS = 14;       // of a token's number in the sort of lists, below its id
 constexpr int LIST = 1024;         // tokens of a list

@@ -285,7 +285,7 @@ __device__ __forceinline__ int2 wave_range(int id) {
 
 // Smallest and largest document of each 64 keys, and whether some are of
 // none: what the walks below need of documents, at a 64th of the reads.
-// A launch: 3 us for 4 x 4096 keys.
+// A launch: 3 to 5 us for 4 x 4096 keys.
 template <typename T>
 __global__ __launch_bounds__(64) void ranges_k(StreamArgs g) {
     const int nr = (g.K + STREAM_RANGE - 1) / STREAM_RANGE, b = (int)blockIdx.x / nr, e = (int)blockIdx.x - b * nr;
@@ -329,19 +329,21 @@ __device__ __forceinline__ void place(int lid, int nz, int& tile, int& z) {
 // rows' sums and two waves fit a SIMD, of which one multiplies while the
 // other takes exponentials.  A third pair of tiles in flight changes nothing
 // (126 us with and without, heads of 64); what bounds it are the vector
-// instructions of the softmax and the products' latency, with capped scores
-// the vector unit (68 % busy: an exponential and a reciprocal more for each).
+// instructions of the softmax (59 % of the vector unit's time) and the products'
+// latency, with capped scores the vector unit (69 %: an exponential and a
+// reciprocal more for each).
 // 4 x 4096 tokens in documents of about 700, 16 heads of 64: 126 us, 0.40
 // PFLOP/s of the pairs that are seen; 8192 causal tokens, capped, 16 heads of
-// 128: 420 us, 0.65; 500 queries behind up to 4096 keys, 16 heads of 96: 39.
+// 128: 375 us, 0.73; 500 queries behind up to 4096 keys, 16 heads of 96: 39.
 // WQ = 1, few rows: reading the keys is what takes time.  Each wave copies
 // its own 32 keys of a step and waits for nobody else; tiles are asked for as
-// soon as they have been read.  Two blocks fit a CU (64 KB of LDS, one pair of
-// tiles a wave for heads of 128, two for smaller ones), so that the one's
-// first and last steps lie beside the other's reads.  64 sequences of up to
-// 8192 keys in 4 key/value heads of 128 (up to 538 MB, all but 5 % of them
-// seen): 105 us, the rate of a large copy; 133 with two pairs of tiles and one
-// block a CU, 165 with tiles that the waves share and a barrier in every step.
+// soon as they have been read.  Two blocks fit a CU (64 KB of LDS: two pairs of
+// tiles a wave up to heads of 64 in 16 bits and 32 in float32, else one pair),
+// so that the one's first and last steps lie beside the other's reads; float32
+// heads above 64 take 128 KB, one block a CU.  64 sequences of 1 to 8192 keys,
+// about uniform, in 4 key/value heads of 128 in bf16 (538 MB at the mean): 103
+// us, 5.2 TB/s; 133 with two pairs of tiles and one block a CU, 165 with tiles
+// that the waves share and a barrier in every step.
 template <typename T, int DP, bool CAP, bool BIAS, int WQ, int NS>
 __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void fwd_k(StreamArgs g) {
     constexpr int WK = 4 / WQ, BM = 32 * WQ, BN = 32 * WK * NS, ND = DP / 32, NC = DP / 16;
@@ -693,7 +695,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void fwd_k(StreamArgs g
 }
 
 // Joins the parts that fwd_k left, in their order: 16 lanes a row.  Bound by
-// reading them: 4 parts of 16000 rows of 96, 25 MB, in 6.5 us.
+// reading them: 4 parts of 16000 rows of 96, 25 MB, in 7 us.
 template <typename T>
 __global__ __launch_bounds__(NT) void join_k(StreamArgs g) {
     const int64_t n = (int64_t)g.B * g.H * g.J, zr = ((int64_t)blockIdx.x * NT + threadIdx.x) >> 4;
@@ -847,7 +849,8 @@ template <typename T> __device__ __forceinline__ float score_grad(float p, float
 // Four products of the formula's five are here.  Bound by the registers: dK,
 // dV and the operands allow two waves a SIMD, whose exponentials, conversions
 // and LDS reads hide half of the products.  8192 causal tokens, capped, 16
-// heads of 128 over 4 key/value heads: 785 us, 0.70 PFLOP/s (QH = 1: 975).
+// heads of 128 over 4 key/value heads: 685 us, 0.80 PFLOP/s, in a row of steps;
+// alone on an idle card 785 (QH = 1: 975).
 template <typename T, int DP, int QH> struct DkvTiles {
     static constexpr int BQ = 64, TB = BQ * Tile<T, DP>::PITCH;
     static constexpr int KT = QH == 2 ? STREAM_KEYS * Tile<T, DP>::PITCH : 0;  // of K, and of V
@@ -1153,7 +1156,7 @@ __global__ __launch_bounds__(NT) void dkv_join_k(StreamArgs g) {
 // forward does.  Three products, of which two form the probabilities' and
 // their gradients' sums again: that is the price of writing no J x K tensor
 // and adding nothing atomically.  8192 causal tokens, capped, 16 heads of
-// 128: 575 us, 0.72 PFLOP/s.
+// 128: 522 us, 0.79 PFLOP/s, in a row of steps.
 template <typename T, int DP> struct DqTiles {
     static constexpr int BN = 64, TB = BN * Tile<T, DP>::PITCH;
     static constexpr int LDS = 4 * TB + 2 * BN * 4 + 4 * 8;  // two pairs of tiles, documents of the keys, of the waves' rows
@@ -1367,9 +1370,9 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void dq_k(StreamArgs g)
 }
 // Both in one launch, so that the end of the one fills with the other:
 // blocks 0 .. nk - 1 (the longer ones) do keys, the others rows.  4 x 4096
-// tokens in documents of about 700, 16 heads of 64: 345 us, 0.52 PFLOP/s of
+// tokens in documents of about 700, 16 heads of 64: 333 us, 0.54 PFLOP/s of
 // the seven products; 3 x 1531 causal tokens with distances in fp16, 12 heads
-// of 64: 70.
+// of 64: 70 to 75.
 template <typename T, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NT, DP <= 64 && sizeof(T) == 2 ? 2 : 1) void dkv_dq_k(StreamArgs g, int nk) {
     constexpr int A = DkvTiles<T, DP, 1>::LDS, B = DqTiles<T, DP>::LDS;
