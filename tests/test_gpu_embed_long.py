@@ -9,6 +9,15 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda"
 
 
+@pytest.fixture(autouse=True)
+def float32_by_default():
+    # (other test modules may have set another default type)
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 def room(gib):
     torch.cuda.empty_cache()
     if torch.cuda.mem_get_info()[0] < gib << 30:

@@ -9,6 +9,15 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda"
 
 
+@pytest.fixture(autouse=True)
+def float32_by_default():
+    # (other test modules may have set another default type)
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 def batch(tokens, V, I, seed):
     g = torch.Generator(device=DEV).manual_seed(seed)
     ids = torch.randint(0, V, (tokens,), generator=g, device=DEV, dtype=torch.int32)
