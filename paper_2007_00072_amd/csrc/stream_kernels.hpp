@@ -619,7 +619,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 2 : 1) void fwd_k(StreamArgs g
         nxt = then;
         nxt_mixed = then_mixed;
     }
-    m = fmaf(m, f, sc.offset - UP);  // from here in units of log2
+    m = sc.offset - fmaf(-m, f, UP);  // from here in units of log2 (what the sums are relative to, as rounded)
     if (hi == 0) {  // a row that sees nothing
         m = -INFINITY;
         l = 0.f;

@@ -54,3 +54,56 @@ def test_values_of_one_sign_over_a_head(J, K, H, G, P, size, cap):
         torch.cuda.synchronize()
         for n, x in zip(("out", "dq", "dk", "dv"), (out, *grads)):
             check(n, x, want[n])
+
+
+def test_a_large_value_behind_a_long_sequence():
+    # (the largest |v| is looked for in groups of keys, which grow with the sequence)
+    J, K, P, half = 5, 70001, 16, torch.float16
+    g = torch.Generator().manual_seed(2)
+    q, v, dout = torch.randn(1, J, 1, P, generator=g), torch.randn(1, K, 1, P, generator=g), torch.ones(1, J, 1, P)
+    k = torch.zeros(1, K, 1, P)
+    k[:, -2:] = 4.0 * q.mean(1, keepdim=True)
+    v[:, -1], v[:, -2] = 50000.0, -50000.0
+    q, k, v, dout = q.to(half), k.to(half), v.to(half), (dout * 2.0 ** -12).to(half)
+    want = reference(q, k, v, dout, scaler=8.0)
+    d = [x.to(DEV) for x in (q, k, v)]
+    a = runner.Attention(*d, scaler=8.0)
+    out = a.forward(*d)
+    grads = a.backward(*d, out, dout.to(DEV))
+    torch.cuda.synchronize()
+    # (as above: 2^s more under fp16's normal numbers)
+    s = float(torch.floor(torch.log2(P * v.double().abs().max()))) - 15
+    more = 2.0 ** -24 * 2.0 ** -12 * (2 ** s - 1) * 8.0
+    want["dq"] = (want["dq"][0], want["dq"][1] + more * k.double().abs().sum(1, keepdim=True))
+    want["dk"] = (want["dk"][0], want["dk"][1] + more * q.double().abs().sum(1, keepdim=True))
+    for n, x in zip(("out", "dq", "dk", "dv"), (out, *grads)):
+        check(n, x, want[n])
+
+
+def test_graph_replays():
+    # the step's largest |dout| and |v| are found anew in every replay
+    B, L, H, G, P = 2, 300, 4, 2, 64
+    g = torch.Generator().manual_seed(3)
+    sets = [[(torch.randn(B, L, n, P, generator=g) * std).half().to(DEV) for n, std in ((H, 1), (G, 1), (G, sv), (H, sd))]
+            for sv, sd in ((1.0, 1.0), (5000.0, 1e-3), (1e-3, 100.0))]
+    a = runner.Attention(*sets[0][:3], causal=True)
+
+    def step(q, k, v, dout):
+        out = a.forward(q, k, v)
+        return (out, *a.backward(q, k, v, out, dout))
+
+    want = [[t.clone() for t in step(*s)] for s in sets]
+    held = [t.clone() for t in sets[0]]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(*held)
+    for i in (1, 0, 2, 1):
+        for x, y in zip(held, sets[i]):
+            x.copy_(y)
+        for t in got:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want[i]))
+        assert all(torch.equal(x, y) for x, y in zip(step(*sets[i]), want[i]))

@@ -58,3 +58,22 @@ def test_gradient_of_many_tokens():
     e.backward(ids, dy.view(tokens, I))
     torch.cuda.synchronize()
     assert torch.equal(e.grad, want)
+
+
+@pytest.mark.parametrize("V", [2 ** 18 - 1, 2 ** 18, 300007, 2 ** 24 + 5])
+@pytest.mark.parametrize("tokens", [1, 300, 1025, 5000])
+def test_large_vocabularies(V, tokens):
+    # (ids past the bits that the sort of lists has)
+    I = 8
+    g = torch.Generator(device=DEV).manual_seed(V % 1000 + tokens)
+    ids = torch.randint(0, V, (tokens,), generator=g, device=DEV, dtype=torch.int32)
+    ids[::3] = V - 1
+    ids[1::7] = V
+    dy = torch.randint(-8, 9, (tokens, I), generator=g, device=DEV).half()
+    table = (torch.arange(V, device=DEV, dtype=torch.int32)[:, None] % 2048 + torch.zeros(I, device=DEV)).half()
+    e = runner.Embedding(table)
+    inside = (ids < V)[:, None]
+    assert torch.equal(e.forward(ids), torch.where(inside, table[ids.long().clamp(max=V - 1)], torch.zeros((), device=DEV).half()))
+    e.grad.fill_(float("nan"))
+    want = torch.zeros(V, I, device=DEV).index_add_(0, ids.long().clamp(max=V - 1), torch.where(inside, dy.float(), 0.0))
+    assert torch.equal(e.backward(ids, dy), want)
