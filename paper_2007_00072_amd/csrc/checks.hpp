@@ -1,6 +1,8 @@
 // Argument checks of the C entry points.
 #pragma once
 
+#include <initializer_list>
+
 #include "internal.hpp"
 
 namespace dm {
@@ -10,6 +12,13 @@ inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline int check_ptr(const void* p, const char* name) {
     if (!p) return set_error(DM_ERR_ARG, "%s is NULL", name);
     if (!aligned16(p)) return set_error(DM_ERR_ARG, "%s is not 16-byte aligned", name);
+    return DM_OK;
+}
+
+// an output that begins where an input (or another output) does
+inline int check_apart(const void* out, const char* name, std::initializer_list<const void*> others) {
+    for (const void* p : others)
+        if (out && out == p) return set_error(DM_ERR_ARG, "%s aliases another tensor of the call", name);
     return DM_OK;
 }
 

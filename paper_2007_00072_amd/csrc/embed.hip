@@ -537,6 +537,7 @@ int embed_fwd(int32_t dtype, int64_t tokens, int32_t vocab, int32_t cols, const 
     DM_TRY(check_embed(dtype, tokens, vocab, cols, scale));
     if (tokens == 0) return DM_OK;
     DM_TRY(check_ptr(ids, "ids")); DM_TRY(check_ptr(table, "table")); DM_TRY(check_ptr(y, "y"));
+    DM_TRY(check_apart(y, "y", {ids, table}));
     const hipStream_t st = S(stream);
     if (dtype == DM_F16) launch_fwd<half_t>(tokens, vocab, cols, ids, table, scale, y, st);
     else if (dtype == DM_BF16) launch_fwd<bf16_t>(tokens, vocab, cols, ids, table, scale, y, st);
@@ -555,6 +556,7 @@ int embed_bwd(int32_t dtype, int64_t tokens, int32_t vocab, int32_t cols, const 
     const size_t need = embed_ws_bytes(tokens, vocab, cols);
     if (ws_bytes < need) return set_error(DM_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws_bytes, need);
     if (need) DM_TRY(check_ptr(ws, "ws"));
+    if (tokens > 0) DM_TRY(check_apart(dtable, "dtable", {ids, dy}));
     const hipStream_t st = S(stream);
     const int64_t n = (int64_t)vocab * cols;
     // zeros: blocks of 64 KB, up to four for each of the 256 CUs

@@ -233,6 +233,8 @@ int attn_fwd(const dm_attn_desc* d, const void* q, const void* k, const void* v,
     if (saved) DM_TRY(check_ptr(saved, "saved"));
     if (ws_bytes < s.fwd) return set_error(DM_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws_bytes, s.fwd);
     if (s.fwd) DM_TRY(check_ptr(ws, "ws"));
+    if (d->K > 0) DM_TRY(check_apart(out, "out", {k, v}));
+    DM_TRY(check_apart(out, "out", {q, saved}));
     StreamArgs a = args_of(*d);
     a.q = rows_of(q, d->q, d->J, d->P); a.o = rows_of(out, d->out, d->J, d->P);
     a.k = rows_of(k, d->k, d->K, d->P); a.v = rows_of(v, d->v, d->K, d->P);
@@ -273,6 +275,16 @@ int attn_bwd(const dm_attn_desc* d, const void* q, const void* k, const void* v,
     }
     if (ws_bytes < s.bwd) return set_error(DM_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws_bytes, s.bwd);
     if (s.bwd) DM_TRY(check_ptr(ws, "ws"));
+    // (of axes without elements the pointers say nothing)
+    const void* rows = d->J > 0 ? dq : nullptr;
+    if (d->J > 0) DM_TRY(check_apart(dq, "dq", {q, out, dout, saved}));
+    if (d->K > 0) {
+        DM_TRY(check_apart(dk, "dk", {k, v, rows}));
+        DM_TRY(check_apart(dv, "dv", {k, v, dk, rows}));
+        if (d->J > 0) DM_TRY(check_apart(dk, "dk", {q, out, dout, saved}));
+        if (d->J > 0) DM_TRY(check_apart(dv, "dv", {q, out, dout, saved}));
+        if (d->J > 0) DM_TRY(check_apart(dq, "dq", {k, v}));
+    }
     StreamArgs a = args_of(*d);
     a.q = rows_of(q, d->q, d->J, d->P); a.o = rows_of(out, d->out, d->J, d->P);
     a.k = rows_of(k, d->k, d->K, d->P); a.v = rows_of(v, d->v, d->K, d->P);

@@ -125,6 +125,15 @@ def _launch(device, entry, *args):
     return stream
 
 
+def _apart(groups) -> None:
+    """Contiguous tensors of {name: tensors} that are written by one call: no two share memory."""
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), n)
+                   for n, ts in groups.items() if ts is not None for t in ts if t.numel())
+    for (_, end, a), (begin, _, b) in zip(spans, spans[1:]):
+        if begin < end:
+            raise ValueError(f"{a} and {b}: two tensors share memory")
+
+
 def _code(dtype: torch.dtype) -> int:
     for n, t in TORCH_DTYPES.items():
         if t == dtype:
@@ -281,7 +290,8 @@ class AdamW:
     weights; None: none).  States are made here (zeros: before the first
     step) in fp32 or, with state_bits=8, as e4m3 codes with a scale for
     each 256 elements, unless given (m, v, and for 8 bits m_scale, v_scale:
-    lists of flat tensors).  decay: one value or one for each tensor."""
+    lists of flat tensors).  No two of all these share memory.  decay: one
+    value or one for each tensor."""
 
     def __init__(self, params: Sequence[torch.Tensor], *, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
                  eps: float = 1e-8, decay=0.0, master="auto", state_bits: int = 32, m=None, v=None, m_scale=None,
@@ -294,8 +304,6 @@ class AdamW:
             state_bits = 32 if m[0].dtype == torch.float32 else 8
         self.params = [_dense("param", p, self.dtype, p.shape, self.device) for p in params]
         self._shapes = [p.shape for p in params]
-        if len({p.data_ptr() for p in params if p.numel()}) < sum(1 for p in params if p.numel()):
-            raise ValueError("a parameter is listed twice")
         if isinstance(master, str):
             master = [p.float() for p in params] if self.dtype != torch.float32 else None
         sd = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
@@ -318,6 +326,8 @@ class AdamW:
         self.v = states("v", v, sd, torch.Tensor.numel)
         self.m_scale = states("m_scale", m_scale, torch.float32, blocks) if state_bits == 8 else None
         self.v_scale = states("v_scale", v_scale, torch.float32, blocks) if state_bits == 8 else None
+        _apart({"param": self.params, "master": self.master, "m": self.m, "v": self.v, "m_scale": self.m_scale,
+                "v_scale": self.v_scale})
         decay = [float(decay)] * len(params) if isinstance(decay, (int, float)) else [float(x) for x in decay]
         none = [None] * len(params)
         rows = zip(self.params, self.master or none, none, self.m, self.v, self.m_scale or none, self.v_scale or none,

@@ -8,7 +8,7 @@ import sys
 from test_abi_hostsan import ROOT, hostsan_lib  # noqa: F401  (a fixture)
 
 FILES = ("test_operators_cpu.py", "test_grids_cpu.py", "test_attention_forms_cpu.py", "test_optimizer_range_cpu.py",
-         "test_owners_devices_cpu.py")
+         "test_owners_devices_cpu.py", "test_aliases_cpu.py")
 
 
 def test_refusals_clean_under_asan_ubsan(hostsan_lib):  # noqa: F811
