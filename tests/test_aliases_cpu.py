@@ -56,11 +56,11 @@ def test_embedding():
 
 
 def test_optimizer_owner():
-    x = torch.zeros(4096)
+    x = torch.zeros(4000)
     with pytest.raises(ValueError, match="share memory"):
-        runner.AdamW([x[:1024], x[1000:2000]])
+        runner.AdamW([x[:1000], x[996:1996]])
     with pytest.raises(ValueError, match="share memory"):
-        runner.AdamW([x[:1024], x[1024:2048]], m=[torch.zeros(1024)] * 2)
+        runner.AdamW([x[:1000], x[1000:2000]], m=[torch.zeros(1000)] * 2)
     with pytest.raises(ValueError, match="share memory"):
         runner.AdamW([x[:16].half()], master=[x[:16]], m=[x[8:24]], v=[torch.zeros(16)])
-    runner.AdamW([x[:1024], x[1024:2048], x[:0]], m=[x[2048:3072], x[3072:], torch.zeros(0)])
+    runner.AdamW([x[:1000], x[1000:2000], x[:0]], m=[x[2000:3000], x[3000:], torch.zeros(0)])

@@ -28,7 +28,8 @@ def plain(ids, dy, V):
     return torch.zeros(V, dy.shape[1], device=DEV).index_add_(0, ids.long(), dy.float())  # (whole numbers: exact)
 
 
-def test_outgrown_workspaces_are_given_back():
+@pytest.mark.parametrize("where", ["side", "default", "both"])
+def test_outgrown_workspaces_are_given_back(where):
     V, I = 1000, 256
     runs = [batch(n, V, I, n) for n in (20000, 50000, 120000)]
     want = [plain(*r, V) for r in runs]
@@ -37,10 +38,12 @@ def test_outgrown_workspaces_are_given_back():
     e = runner.Embedding(torch.zeros(V, I, dtype=torch.float16, device=DEV))
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
+    streams = {"side": [side], "default": [torch.cuda.current_stream()], "both": [side, torch.cuda.current_stream()]}
     for (ids, dy), w in zip(runs, want):
-        with torch.cuda.stream(side):
-            got = e.backward(ids, dy).clone()
-        torch.cuda.synchronize()
+        for s in streams[where]:
+            with torch.cuda.stream(s):
+                got = e.backward(ids, dy).clone()
+            torch.cuda.synchronize()
         assert torch.equal(got, w)
         del got
     torch.cuda.empty_cache()  # (blocks that wait for another stream are looked at)
